@@ -19,6 +19,8 @@ Modules (each function cites the passage of the paper it follows):
   fusion   reward fusion (Eq. 3) and depth-wise normalisation (Eq. 4)
   prune    width / depth pruning (Sec. 3.4) and the kept-edge set
   objective  clipped GRPO objective value over edges (Eq. 5)
+  train    operators of a policy update: packed attention, modulated LayerNorm,
+           gradient of the objective, AdamW with states in 32 or 8 bits
 
 Pins: see tests/test_oracle_*.py.  Unpinned items are listed in each module's
 header.

@@ -32,6 +32,11 @@ EXPORTS = (
     "br_noise_stream", "br_depth_mask_window", "br_depth_mask_seeded", "br_mix_schedule", "br_fusion_ess", "br_op_gemm", "br_op_attention",
     "br_op_ln_modulate", "br_profile_enable", "br_profile_read",
 )
+# declared in branchrollout_train.h
+TRAIN_EXPORTS = (
+    "br_attention_workspace_bytes", "br_attention_forward", "br_attention_backward", "br_layer_norm_workspace_bytes", "br_layer_norm_forward",
+    "br_layer_norm_backward", "br_edge_rows", "br_grpo_backward_workspace_bytes", "br_grpo_backward", "br_adamw_step", "br_adamw_state_values",
+)
 
 
 class BranchRolloutError(RuntimeError):
@@ -60,7 +65,8 @@ def load():
         raise FileNotFoundError("%s is missing: build it with `python -m paper_2509_06040_amd.build`" % LIB_PATH)
     lib = C.CDLL(LIB_PATH)
     lib.br_last_error.restype = C.c_char_p
-    for name in ("br_workspace_bytes", "br_reward_scratch_bytes", "br_sde_scratch_bytes", "br_sde_static_scratch_limit"):
+    for name in ("br_workspace_bytes", "br_reward_scratch_bytes", "br_sde_scratch_bytes", "br_sde_static_scratch_limit", "br_attention_workspace_bytes",
+                 "br_layer_norm_workspace_bytes", "br_grpo_backward_workspace_bytes"):
         getattr(lib, name).restype = C.c_size_t
     lib.br_tree_free.restype = None
     lib.br_model_free.restype = None
@@ -320,3 +326,181 @@ def profile_read(max_ids=64):
     n = C.c_int32()
     _check(load().br_profile_read(C.c_int32(max_ids), ids, work, ms, launches, C.byref(n)))
     return {ids[i]: (work[i], ms[i], launches[i]) for i in range(n.value)}
+
+
+# ------------------------------------------------------------------------------------------ the operators of a policy update
+class AttnShape(C.Structure):
+    _fields_ = ([(n, C.c_int32) for n in ("dtype", "n_heads", "n_kv_heads", "head_dim", "n_docs", "q_tokens", "k_tokens")] + [("scale", C.c_float)] +
+                [(n, C.c_int64) for n in ("q_stride", "k_stride", "v_stride", "o_stride", "dq_stride", "dk_stride", "dv_stride")] +
+                [("q_off", C.c_void_p), ("k_off", C.c_void_p)])
+
+
+class NormShape(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "rows", "hidden", "n_docs", "n_groups", "mods_stride", "shift_off", "scale_off")] + [("row_off", C.c_void_p), ("group", C.c_void_p)]
+
+
+class EdgeSet(C.Structure):
+    _fields_ = [("D", C.c_int64), ("n_nodes", C.c_int32), ("n_rows", C.c_int32), ("n_edges", C.c_int32), ("n_total", C.c_int32), ("clip_eps", C.c_float),
+                ("edge_ids", C.c_void_p), ("row_parent", C.c_void_p), ("row_first", C.c_void_p), ("row_coef", C.c_void_p)]
+
+
+class AdamwTensor(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("param", "grad", "m", "v", "m_scale", "v_scale", "copy")] + [("n", C.c_int64), ("weight_decay", C.c_double)]
+
+
+class AdamwCfg(C.Structure):
+    _fields_ = [(n, C.c_double) for n in ("lr", "beta1", "beta2", "eps")] + [("step", C.c_int64), ("seed", C.c_uint64), ("grad_dtype", C.c_int32),
+                                                                            ("state_bits", C.c_int32), ("grad_scale", C.c_void_p)]
+
+
+def _dtype(x):
+    name = str(x.dtype)
+    assert name in ("torch.float32", "torch.bfloat16"), name
+    return F32 if name == "torch.float32" else BF16
+
+
+def _token_stride(x):
+    """Elements between tokens of a [tokens, heads, head_dim] tensor whose heads are adjacent."""
+    tokens, heads, d = x.shape
+    assert tokens == 0 or (x.stride(2) == 1 and (heads == 1 or x.stride(1) == d)), "heads of a token must be adjacent"
+    return x.stride(0) if tokens > 1 else heads * d
+
+
+def _flat(x, dtype=None):
+    """Device pointer of a contiguous tensor, as a number."""
+    if x is None:
+        return None
+    assert x.is_contiguous() and (dtype is None or str(x.dtype) == dtype), (x.stride(), x.dtype)
+    return x.data_ptr()
+
+
+def _room(workspace):
+    return (C.c_void_p(0), C.c_size_t(0)) if workspace is None else (_p(workspace), C.c_size_t(workspace.numel() * workspace.element_size()))
+
+
+def _attn_shape(q, k, v, o, q_off, k_off, scale, dq=None, dk=None, dv=None):
+    assert q.dtype == k.dtype == v.dtype == o.dtype and k.shape == v.shape and q.shape == o.shape and q.shape[2] == k.shape[2], "shapes or types differ"
+    assert q_off.shape == k_off.shape and q_off.dim() == 1, "one offset more than documents"
+    s = AttnShape(_dtype(q), q.shape[1], k.shape[1], q.shape[2], q_off.shape[0] - 1, q.shape[0], k.shape[0], 0.0 if scale is None else scale,
+                  _token_stride(q), _token_stride(k), _token_stride(v), _token_stride(o), 0, 0, 0, _flat(q_off, "torch.int32"), _flat(k_off, "torch.int32"))
+    if dq is not None:
+        assert dq.shape == q.shape and dk.shape == k.shape and dv.shape == v.shape and dq.dtype == dk.dtype == dv.dtype == q.dtype, "shapes or types differ"
+        s.dq_stride, s.dk_stride, s.dv_stride = _token_stride(dq), _token_stride(dk), _token_stride(dv)
+    return s
+
+
+def attention_workspace_bytes(q, k, v, q_off, k_off, backward):
+    s = _attn_shape(q, k, v, q, q_off, k_off, None, *((q, k, v) if backward else ()))
+    return load().br_attention_workspace_bytes(C.byref(s), C.c_int32(1 if backward else 0))
+
+
+def attention_forward(q, k, v, q_off, k_off, out, lse, workspace=None, scale=None):
+    """q, out [tokens, heads, head_dim], k, v [tokens, kv heads, head_dim] (tokens may be strided), offsets int32 [documents + 1], lse [heads, tokens] fp32."""
+    s = _attn_shape(q, k, v, out, q_off, k_off, scale)
+    assert tuple(lse.shape) == (q.shape[1], q.shape[0])
+    _check(load().br_attention_forward(C.byref(s), C.c_void_p(q.data_ptr()), C.c_void_p(k.data_ptr()), C.c_void_p(v.data_ptr()), C.c_void_p(out.data_ptr()),
+                                       C.c_void_p(_flat(lse, "torch.float32")), *_room(workspace), _stream()))
+
+
+def attention_backward(dout, q, k, v, out, lse, q_off, k_off, dq, dk, dv, workspace, scale=None):
+    s = _attn_shape(q, k, v, out, q_off, k_off, scale, dq, dk, dv)
+    assert dout.shape == out.shape and dout.dtype == out.dtype and _token_stride(dout) == s.o_stride, "dout must be laid out as out"
+    assert tuple(lse.shape) == (q.shape[1], q.shape[0])
+    _check(load().br_attention_backward(C.byref(s), *[C.c_void_p(x.data_ptr()) for x in (dout, q, k, v, out)], C.c_void_p(_flat(lse, "torch.float32")),
+                                        *[C.c_void_p(x.data_ptr()) for x in (dq, dk, dv)], *_room(workspace), _stream()))
+
+
+def _norm_shape(x, y, mods, shift_off, scale_off, row_off, group):
+    assert x.shape == y.shape and group.shape[0] == row_off.shape[0] - 1, "shapes differ"
+    return NormShape(_dtype(y), x.shape[0], x.shape[1], group.shape[0], mods.shape[0], mods.shape[1], shift_off, scale_off, _flat(row_off, "torch.int32"),
+                     _flat(group, "torch.int32"))
+
+
+def layer_norm_workspace_bytes(x, dout, mods, shift_off, scale_off, row_off, group):
+    s = _norm_shape(x, dout, mods, shift_off, scale_off, row_off, group)
+    return load().br_layer_norm_workspace_bytes(C.byref(s))
+
+
+def layer_norm_forward(x, mods, shift_off, scale_off, row_off, group, out, mean=None, rstd=None):
+    s = _norm_shape(x, out, mods, shift_off, scale_off, row_off, group)
+    assert mean is None or mean.numel() == rstd.numel() == x.shape[0]
+    f = "torch.float32"
+    _check(load().br_layer_norm_forward(C.byref(s), C.c_void_p(_flat(x, f)), C.c_void_p(_flat(mods, f)), C.c_void_p(_flat(out)), C.c_void_p(_flat(mean, f)), C.c_void_p(_flat(rstd, f)),
+                                        _stream()))
+
+
+def layer_norm_backward(dout, x, mean, rstd, mods, shift_off, scale_off, row_off, group, residual, dx, dmods, workspace):
+    s = _norm_shape(x, dout, mods, shift_off, scale_off, row_off, group)
+    assert dx.shape == x.shape and dmods.shape == mods.shape and mean.numel() == rstd.numel() == x.shape[0] and (residual is None or residual.shape == x.shape)
+    f = "torch.float32"
+    _check(load().br_layer_norm_backward(C.byref(s), C.c_void_p(_flat(dout)), *[C.c_void_p(_flat(t, f)) for t in (x, mean, rstd, mods, residual, dx, dmods)], *_room(workspace),
+                                         _stream()))
+
+
+def edge_rows(tree, sched, D, edge_ids):
+    """-> (row_parent, row_first, row_coef [rows, 4]): host tables of the edges' distinct parents."""
+    s = make_sched(sched)
+    e, ep = _h(edge_ids, np.int32)
+    n = len(e)
+    parent, first, coef, rows = np.zeros(max(n, 1), np.int32), np.zeros(n + 1, np.int32), np.zeros((max(n, 1), 4), np.float64), C.c_int32()
+    _check(load().br_edge_rows(tree._h, C.byref(s), C.c_int64(D), ep, C.c_int32(n), *[a.ctypes.data_as(C.c_void_p) for a in (parent, first, coef)], C.byref(rows)))
+    r = rows.value
+    return parent[:r].copy(), first[:r + 1].copy(), coef[:r].copy()
+
+
+def _edge_set(z_nodes, v_rows, edge_ids, row_parent, row_first, row_coef, clip_eps, n_total):
+    i32 = "torch.int32"
+    assert z_nodes.shape[1] == v_rows.shape[1] and row_parent.shape[0] == v_rows.shape[0] == row_first.shape[0] - 1 and row_coef.numel() == 4 * row_parent.shape[0], "shapes differ"
+    return EdgeSet(z_nodes.shape[1], z_nodes.shape[0], row_parent.shape[0], edge_ids.shape[0], n_total, clip_eps, _flat(edge_ids, i32), _flat(row_parent, i32), _flat(row_first, i32),
+                   _flat(row_coef, "torch.float64"))
+
+
+def grpo_backward_workspace_bytes(z_nodes, v_rows, edge_ids, row_parent, row_first, row_coef):
+    s = _edge_set(z_nodes, v_rows, edge_ids, row_parent, row_first, row_coef, 0.0, 0)
+    return load().br_grpo_backward_workspace_bytes(C.byref(s))
+
+
+def grpo_backward(z_nodes, v_rows, edge_ids, row_parent, row_first, row_coef, logp_old_nodes, adv_nodes, clip_eps, J, logp_new, grad_v, workspace, clipped=None, n_total=0):
+    s = _edge_set(z_nodes, v_rows, edge_ids, row_parent, row_first, row_coef, clip_eps, n_total)
+    assert grad_v.shape == v_rows.shape and logp_new.shape == edge_ids.shape and logp_old_nodes.numel() == adv_nodes.numel() == z_nodes.shape[0], "shapes differ"
+    f = "torch.float32"
+    _check(load().br_grpo_backward(C.byref(s), *[C.c_void_p(_flat(t, f)) for t in (z_nodes, v_rows, logp_old_nodes, adv_nodes, J, logp_new, grad_v)], C.c_void_p(_flat(clipped)),
+                                   *_room(workspace), _stream()))
+
+
+class AdamW:
+    """The tensors of a network and their optimizer states (lists of equal length; every tensor contiguous).  params fp32; grads all fp32 or all bf16; m, v
+    fp32, or uint8 codes with m_scales, v_scales (fp32, one of 256 elements); copies: bf16 tensors that receive the rounded parameters, or None."""
+
+    def __init__(self, params, grads, m, v, m_scales=None, v_scales=None, copies=None, weight_decay=0.01, lr=1e-4, betas=(0.9, 0.999), eps=1e-8, seed=0, step=0):
+        n = len(params)
+        none = [None] * n
+        bits = 32 if m_scales is None else 8
+        state = "torch.float32" if bits == 32 else "torch.uint8"
+        decay = [weight_decay] * n if isinstance(weight_decay, (int, float)) else list(weight_decay)
+        self.tensors = (AdamwTensor * max(n, 1))()
+        self.n, self._keep = n, (params, grads, m, v, m_scales, v_scales, copies)
+        f = "torch.float32"
+        for i, (p, g, mm, vv, ms, vs, c, w) in enumerate(zip(params, grads, m, v, m_scales or none, v_scales or none, copies or none, decay, strict=True)):
+            k = p.numel()
+            assert g.numel() == mm.numel() == vv.numel() == k and (c is None or c.numel() == k) and (ms is None or ms.numel() == vs.numel() == (k + 255) // 256), "sizes differ"
+            assert g.dtype == grads[0].dtype
+            self.tensors[i] = AdamwTensor(_flat(p, f), _flat(g), _flat(mm, state), _flat(vv, state), _flat(ms, f), _flat(vs, f), _flat(c, "torch.bfloat16"), k, w)
+        self.cfg = AdamwCfg(lr, betas[0], betas[1], eps, step, seed, _dtype(grads[0]) if n else F32, bits, None)
+
+    def step(self, lr=None, grad_scale=None):
+        """One step; grad_scale: a device tensor of one fp32 factor of all gradients, or None."""
+        if lr is not None:
+            self.cfg.lr = lr
+        self.cfg.step += 1
+        self.cfg.grad_scale = _flat(grad_scale, "torch.float32")
+        code = load().br_adamw_step(C.byref(self.cfg), self.tensors, C.c_int32(self.n), _stream())
+        if code != 0:
+            self.cfg.step -= 1
+        _check(code)
+
+    def state_values(self, m_out, v_out):
+        """The values that states in 8 bits stand for, into fp32 tensors."""
+        pointers = [(C.c_void_p * max(self.n, 1))(*[_flat(x, "torch.float32") for x in out]) for out in (m_out, v_out)]
+        assert all(x.numel() == t.n for out in (m_out, v_out) for x, t in zip(out, self.tensors))
+        _check(load().br_adamw_state_values(self.tensors, C.c_int32(self.n), *pointers, _stream()))

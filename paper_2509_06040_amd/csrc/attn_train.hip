@@ -1,0 +1,402 @@
+// Attention over packed documents with its backward pass: the forms that hold for every type and head dim.
+//
+// A wavefront keeps 16 rows of one side in registers (queries forward and for dq, keys for dk and dv) and walks the rows of the other side in tiles
+// that the workgroup stages in LDS.  Scores are taken so that a lane holds four rows of the tile for ONE row of its own per block of 16 (C layout of the 16x16
+// matrix instructions); exponentiated, these registers are, without moving, the column operand of the products that contract over the tile's rows, whose row
+// operand is read from LDS transposed.
+#include "dit.h"
+#include "docs.h"
+#include "train.h"
+
+namespace br {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+
+// Operands of a type.  A fragment holds EPL consecutive contraction indices of quarter g of the lanes: a step contracts 4 EPL of them.
+template <typename T>
+struct Op;
+template <>
+struct Op<bf16> {
+  using Frag = bf16x8;
+  static constexpr int EPL = 8;
+  static __device__ inline f32x4 mma(const Frag& a, const Frag& b, const f32x4& c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+};
+template <>
+struct Op<float> {
+  using Frag = f32x4;
+  static constexpr int EPL = 4;
+  static __device__ inline f32x4 mma(const Frag& a, const Frag& b, f32x4 c) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);  // (each takes index 4 g + e from quarter g)
+    return c;
+  }
+};
+
+// A tile of 64 rows of DH values in LDS.  Rows of bf16 lie as they are, their 16-byte chunks permuted per row so that fragments of 16 consecutive rows and
+// transposed reads of eight rows and two chunks both spread over the banks; rows of fp32 are 16 bytes further apart.
+constexpr int TILE_ROWS = 64;
+template <typename T, int DH>
+struct Tile {
+  static constexpr int ROW = DH * (int)sizeof(T) + (sizeof(T) == 4 ? 16 : 0), BYTES = TILE_ROWS * ROW, CH = DH * (int)sizeof(T) / 16;
+  static __device__ inline int chunk(int r, int c) {
+    if constexpr (sizeof(T) == 4) return r * ROW + c * 16;
+    const int f = DH == 128 ? ((r & 7) << 1 | (r >> 3 & 1)) : ((r >> 1 & 3) << 1 | (r >> 3 & 1));
+    return r * ROW + ((c ^ f) << 4);
+  }
+  // rows first .. first + 63 (those from `end` on: zeros) of a matrix with `stride` elements a row
+  static __device__ inline void stage(char* lds, const T* p, size_t stride, int first, int end) {
+    for (int i = threadIdx.x; i < TILE_ROWS * CH; i += 256) {
+      const int r = i / CH, c = i - r * CH;
+      f32x4 v = {0.f, 0.f, 0.f, 0.f};
+      if (first + r < end) v = *reinterpret_cast<const f32x4*>(reinterpret_cast<const char*>(p + (size_t)(first + r) * stride) + c * 16);
+      *reinterpret_cast<f32x4*>(lds + chunk(r, c)) = v;
+    }
+  }
+  // row operand: rows 16 blk + lane % 16, contraction over the channels of step ks
+  static __device__ inline typename Op<T>::Frag rows(const char* lds, int blk, int ks) {
+    const int lane = threadIdx.x & 63;
+    return *reinterpret_cast<const typename Op<T>::Frag*>(lds + chunk(blk * 16 + (lane & 15), ks * 4 + (lane >> 4)));
+  }
+  // row operand: channels 16 d + lane % 16, contraction over the rows of step ks: rows 4 g + e of its blocks of 16
+  static __device__ inline typename Op<T>::Frag cols(const char* lds, int ks, int d) {
+    const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4;
+    if constexpr (sizeof(T) == 2) {
+      // in a group of 16 lanes, lane 4 r + q supplies the address of 8 bytes (4 values of row r) and lane j receives element j of rows 0..3
+      const int r = 4 * g + (l16 >> 2), at = chunk(ks * 32 + r, 2 * d + ((l16 & 3) >> 1)) + 8 * (l16 & 1), at2 = chunk(ks * 32 + 16 + r, 2 * d + ((l16 & 3) >> 1)) + 8 * (l16 & 1);
+      union { s16x4 s[2]; bf16x8 v; } u;
+      u.s[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(lds + at));
+      u.s[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(lds + at2));
+      return u.v;
+    } else {
+      f32x4 v;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = *reinterpret_cast<const float*>(lds + (ks * 16 + 4 * g + e) * ROW + (16 * d + l16) * 4);
+      return v;
+    }
+  }
+};
+
+// Column operands from registers: row `row` of a matrix (below `end`, else zeros), all channels.
+template <typename T, int DH>
+static __device__ inline void own_rows(typename Op<T>::Frag (&f)[DH / (4 * Op<T>::EPL)], const T* p, size_t stride, int row, int end) {
+#pragma unroll
+  for (int ks = 0; ks < DH / (4 * Op<T>::EPL); ++ks) {
+    f[ks] = typename Op<T>::Frag{};
+    if (row < end) f[ks] = *reinterpret_cast<const typename Op<T>::Frag*>(p + (size_t)row * stride + ks * 4 * Op<T>::EPL + (threadIdx.x >> 4 & 3) * Op<T>::EPL);
+  }
+}
+// Step ks of a contraction over the tile's rows: blocks of 16 rows in the C layout, in the type of the operands.
+template <typename T>
+static __device__ inline typename Op<T>::Frag step_of(const f32x4 (&p)[4], int ks) {
+  if constexpr (sizeof(T) == 2) {
+    bf16x8 f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = (bf16)p[2 * ks + (e >> 2)][e & 3];
+    return f;
+  } else {
+    return p[ks];
+  }
+}
+
+__device__ inline float quarters_max(float x) {
+  x = __builtin_elementwise_maximum(x, __shfl_xor(x, 16, 64));
+  return __builtin_elementwise_maximum(x, __shfl_xor(x, 32, 64));
+}
+__device__ inline float quarters_sum(float x) {
+  x += __shfl_xor(x, 16, 64);
+  return x + __shfl_xor(x, 32, 64);
+}
+
+struct AttnArgs {
+  br_attn_shape s;
+  float scale;
+  const void *q, *k, *v, *out, *dout;
+  float *lse, *delta;
+  void *o, *dq, *dk, *dv;
+};
+
+// The keys of the document with the queries of `span`.
+__device__ inline DocSpan other_rows(const int* off, int n, int rows, const DocSpan& span) {
+  DocSpan o{-1, 0, 0};
+  if (span.doc >= 0) o = doc_item(off, n, rows, span.doc + 1);
+  return o;
+}
+
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void packed_attention_kernel(AttnArgs a) {
+  using O = Op<T>;
+  using L = Tile<T, DH>;
+  constexpr int KS = DH / (4 * O::EPL), PS = TILE_ROWS / (4 * O::EPL), DB = DH / 16;
+  __shared__ __attribute__((aligned(16))) char lds[2 * L::BYTES];
+  DocSpan span;
+  int first;
+  if (!doc_tile(a.s.q_off, a.s.n_docs, a.s.q_tokens, 64, blockIdx.x, &span, &first)) return;
+  const DocSpan keys = other_rows(a.s.k_off, a.s.n_docs, a.s.k_tokens, span);
+  const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4, head = blockIdx.y, kv = head / (a.s.n_heads / a.s.n_kv_heads);
+  const int row = first + (threadIdx.x >> 6) * 16 + l16;
+  const T *k = (const T*)a.k + (size_t)kv * DH, *v = (const T*)a.v + (size_t)kv * DH;
+  typename O::Frag q[KS];
+  own_rows<T, DH>(q, (const T*)a.q + (size_t)head * DH, a.s.q_stride, row, span.end);
+  f32x4 o[DB];
+#pragma unroll
+  for (int d = 0; d < DB; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float top = -INFINITY, sum = 0.f;
+  const float unit = a.scale * LOG2E;  // scores in powers of two
+  for (int k0 = keys.first; k0 < keys.end; k0 += TILE_ROWS) {
+    __syncthreads();
+    L::stage(lds, k, a.s.k_stride, k0, keys.end);
+    L::stage(lds + L::BYTES, v, a.s.v_stride, k0, keys.end);
+    __syncthreads();
+    f32x4 p[4];
+    float most = -INFINITY;
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      p[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) p[b] = O::mma(L::rows(lds, b, ks), q[ks], p[b]);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        p[b][r] = k0 + b * 16 + 4 * g + r < keys.end ? p[b][r] * unit : -INFINITY;
+        most = __builtin_elementwise_maximum(most, p[b][r]);
+      }
+    }
+    const float next = __builtin_elementwise_maximum(top, quarters_max(most)), ref = next == -INFINITY ? 0.f : next;
+    const float shrink = __builtin_amdgcn_exp2f(top - ref);
+    float part = 0.f;
+#pragma unroll
+    for (int b = 0; b < 4; ++b)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        p[b][r] = __builtin_amdgcn_exp2f(p[b][r] - ref);
+        part += p[b][r];
+      }
+    sum = sum * shrink + part;
+    top = next;
+#pragma unroll
+    for (int d = 0; d < DB; ++d) o[d] *= shrink;
+#pragma unroll
+    for (int ks = 0; ks < PS; ++ks) {
+      const typename O::Frag pf = step_of<T>(p, ks);
+#pragma unroll
+      for (int d = 0; d < DB; ++d) o[d] = O::mma(L::cols(lds + L::BYTES, ks, d), pf, o[d]);
+    }
+  }
+  sum = quarters_sum(sum);
+  if (row >= span.end) return;
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  T* out = (T*)a.o + (size_t)row * a.s.o_stride + (size_t)head * DH + 4 * g;
+#pragma unroll
+  for (int d = 0; d < DB; ++d) store4(out + 16 * d, o[d][0] * inv, o[d][1] * inv, o[d][2] * inv, o[d][3] * inv);
+  if (g == 0) a.lse[(size_t)head * a.s.q_tokens + row] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * LN2;
+}
+
+// dq, and delta_i = dout_i . out_i for the kernel of dk and dv.
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void packed_attention_dq_kernel(AttnArgs a) {
+  using O = Op<T>;
+  using L = Tile<T, DH>;
+  constexpr int KS = DH / (4 * O::EPL), PS = TILE_ROWS / (4 * O::EPL), DB = DH / 16;
+  __shared__ __attribute__((aligned(16))) char lds[2 * L::BYTES];
+  DocSpan span;
+  int first;
+  if (!doc_tile(a.s.q_off, a.s.n_docs, a.s.q_tokens, 64, blockIdx.x, &span, &first)) return;
+  const DocSpan keys = other_rows(a.s.k_off, a.s.n_docs, a.s.k_tokens, span);
+  const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4, head = blockIdx.y, kv = head / (a.s.n_heads / a.s.n_kv_heads);
+  const int row = first + (threadIdx.x >> 6) * 16 + l16;
+  const T *k = (const T*)a.k + (size_t)kv * DH, *v = (const T*)a.v + (size_t)kv * DH;
+  typename O::Frag q[KS], dout[KS];
+  own_rows<T, DH>(q, (const T*)a.q + (size_t)head * DH, a.s.q_stride, row, span.end);
+  own_rows<T, DH>(dout, (const T*)a.dout + (size_t)head * DH, a.s.o_stride, row, span.end);
+  float delta = 0.f, ref = INFINITY;  // (a query without keys, or that is not there: probabilities of zero)
+  {
+    typename O::Frag out[KS];
+    own_rows<T, DH>(out, (const T*)a.out + (size_t)head * DH, a.s.o_stride, row, span.end);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+      for (int e = 0; e < O::EPL; ++e) delta = fmaf((float)dout[ks][e], (float)out[ks][e], delta);
+    delta = quarters_sum(delta);
+    if (row < span.end) {
+      const size_t at = (size_t)head * a.s.q_tokens + row;
+      if (g == 0) a.delta[at] = delta;
+      const float lse = a.lse[at];
+      if (lse != -INFINITY) ref = lse * LOG2E;
+    }
+  }
+  f32x4 dq[DB];
+#pragma unroll
+  for (int d = 0; d < DB; ++d) dq[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const float unit = a.scale * LOG2E;
+  for (int k0 = keys.first; k0 < keys.end; k0 += TILE_ROWS) {
+    __syncthreads();
+    L::stage(lds, k, a.s.k_stride, k0, keys.end);
+    L::stage(lds + L::BYTES, v, a.s.v_stride, k0, keys.end);
+    __syncthreads();
+    f32x4 ds[4];
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      f32x4 s = {0.f, 0.f, 0.f, 0.f}, dp = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        s = O::mma(L::rows(lds, b, ks), q[ks], s);
+        dp = O::mma(L::rows(lds + L::BYTES, b, ks), dout[ks], dp);
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float p = __builtin_amdgcn_exp2f(fmaf(s[r], unit, -ref));
+        ds[b][r] = k0 + b * 16 + 4 * g + r < keys.end ? p * (dp[r] - delta) : 0.f;
+      }
+    }
+#pragma unroll
+    for (int ks = 0; ks < PS; ++ks) {
+      const typename O::Frag f = step_of<T>(ds, ks);
+#pragma unroll
+      for (int d = 0; d < DB; ++d) dq[d] = O::mma(L::cols(lds, ks, d), f, dq[d]);
+    }
+  }
+  if (row >= span.end) return;
+  T* to = (T*)a.dq + (size_t)row * a.s.dq_stride + (size_t)head * DH + 4 * g;
+#pragma unroll
+  for (int d = 0; d < DB; ++d) store4(to + 16 * d, dq[d][0] * a.scale, dq[d][1] * a.scale, dq[d][2] * a.scale, dq[d][3] * a.scale);
+}
+
+// dk and dv of 64 keys, over the queries of all heads that share them.
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void packed_attention_dkv_kernel(AttnArgs a) {
+  using O = Op<T>;
+  using L = Tile<T, DH>;
+  constexpr int KS = DH / (4 * O::EPL), PS = TILE_ROWS / (4 * O::EPL), DB = DH / 16;
+  __shared__ __attribute__((aligned(16))) char lds[2 * L::BYTES];
+  __shared__ __attribute__((aligned(16))) float refs[2 * TILE_ROWS];  // lse in powers of two (infinite where there is no query), delta
+  DocSpan span;
+  int first;
+  if (!doc_tile(a.s.k_off, a.s.n_docs, a.s.k_tokens, 64, blockIdx.x, &span, &first)) return;
+  const DocSpan queries = other_rows(a.s.q_off, a.s.n_docs, a.s.q_tokens, span);
+  const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4, kv = blockIdx.y, share = a.s.n_heads / a.s.n_kv_heads;
+  const int row = first + (threadIdx.x >> 6) * 16 + l16;
+  typename O::Frag k[KS], v[KS];
+  own_rows<T, DH>(k, (const T*)a.k + (size_t)kv * DH, a.s.k_stride, row, span.end);
+  own_rows<T, DH>(v, (const T*)a.v + (size_t)kv * DH, a.s.v_stride, row, span.end);
+  f32x4 dk[DB], dv[DB];
+#pragma unroll
+  for (int d = 0; d < DB; ++d) dk[d] = dv[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const float unit = a.scale * LOG2E;
+  for (int head = kv * share; head < (kv + 1) * share; ++head) {
+    const T *q = (const T*)a.q + (size_t)head * DH, *dout = (const T*)a.dout + (size_t)head * DH;
+    for (int q0 = queries.first; q0 < queries.end; q0 += TILE_ROWS) {
+      __syncthreads();
+      L::stage(lds, q, a.s.q_stride, q0, queries.end);
+      L::stage(lds + L::BYTES, dout, a.s.o_stride, q0, queries.end);
+      if (threadIdx.x < TILE_ROWS) {
+        const int i = q0 + threadIdx.x;
+        const size_t at = (size_t)head * a.s.q_tokens + i;
+        const float lse = i < queries.end ? a.lse[at] : -INFINITY;
+        refs[threadIdx.x] = lse == -INFINITY ? INFINITY : lse * LOG2E;
+        refs[TILE_ROWS + threadIdx.x] = i < queries.end ? a.delta[at] : 0.f;
+      }
+      __syncthreads();
+      f32x4 p[4], ds[4];
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        f32x4 s = {0.f, 0.f, 0.f, 0.f}, dp = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          s = O::mma(L::rows(lds, b, ks), k[ks], s);
+          dp = O::mma(L::rows(lds + L::BYTES, b, ks), v[ks], dp);
+        }
+        const f32x4 ref = *reinterpret_cast<const f32x4*>(refs + b * 16 + 4 * g), delta = *reinterpret_cast<const f32x4*>(refs + TILE_ROWS + b * 16 + 4 * g);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          p[b][r] = __builtin_amdgcn_exp2f(fmaf(s[r], unit, -ref[r]));
+          ds[b][r] = p[b][r] * (dp[r] - delta[r]);
+        }
+      }
+#pragma unroll
+      for (int ks = 0; ks < PS; ++ks) {
+        const typename O::Frag pf = step_of<T>(p, ks), df = step_of<T>(ds, ks);
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+          dv[d] = O::mma(L::cols(lds + L::BYTES, ks, d), pf, dv[d]);
+          dk[d] = O::mma(L::cols(lds, ks, d), df, dk[d]);
+        }
+      }
+    }
+  }
+  if (row >= span.end) return;
+  T* tk = (T*)a.dk + (size_t)row * a.s.dk_stride + (size_t)kv * DH + 4 * g;
+  T* tv = (T*)a.dv + (size_t)row * a.s.dv_stride + (size_t)kv * DH + 4 * g;
+#pragma unroll
+  for (int d = 0; d < DB; ++d) {
+    store4(tk + 16 * d, dk[d][0] * a.scale, dk[d][1] * a.scale, dk[d][2] * a.scale, dk[d][3] * a.scale);
+    store4(tv + 16 * d, dv[d][0], dv[d][1], dv[d][2], dv[d][3]);
+  }
+}
+
+static AttnArgs attn_args(const br_attn_shape& s) {
+  AttnArgs a{};
+  a.s = s;
+  a.scale = s.scale > 0.f ? s.scale : (float)(1.0 / sqrt((double)s.head_dim));
+  return a;
+}
+
+// f(T, DH)
+template <typename F>
+static void attn_form(const br_attn_shape& s, F f) {
+#define BR_D(n) std::integral_constant<int, n>{}
+  if (s.dtype == BR_BF16) {
+    if (s.head_dim == 64) f(bf16{}, BR_D(64));
+    else f(bf16{}, BR_D(128));
+  } else {
+    if (s.head_dim == 16) f(float{}, BR_D(16));
+    else if (s.head_dim == 32) f(float{}, BR_D(32));
+    else if (s.head_dim == 64) f(float{}, BR_D(64));
+    else f(float{}, BR_D(128));
+  }
+#undef BR_D
+}
+
+size_t attn_train_workspace(const br_attn_shape& s, bool backward) { return backward ? align_up((size_t)s.n_heads * s.q_tokens * 4, 256) : 0; }
+
+br_status launch_attn_train_forward(const br_attn_shape& s, const void* q, const void* k, const void* v, void* out, float* lse, void* ws, hipStream_t st) {
+  AttnArgs a = attn_args(s);
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.o = out;
+  a.lse = lse;
+  const dim3 grid((unsigned)doc_tiles_most(s.n_docs, s.q_tokens, 64), s.n_heads);
+  attn_form(s, [&](auto Tc, auto Dc) { hipLaunchKernelGGL((packed_attention_kernel<decltype(Tc), decltype(Dc)::value>), grid, dim3(256), 0, st, a); });
+  BR_LAUNCH_CHECK();
+  return BR_OK;
+}
+
+br_status launch_attn_train_backward(const br_attn_shape& s, const void* dout, const void* q, const void* k, const void* v, const void* out, const float* lse, void* dq, void* dk,
+                                     void* dv, void* ws, hipStream_t st) {
+  AttnArgs a = attn_args(s);
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.out = out;
+  a.dout = dout;
+  a.lse = const_cast<float*>(lse);
+  a.delta = reinterpret_cast<float*>(ws);
+  a.dq = dq;
+  a.dk = dk;
+  a.dv = dv;
+  const dim3 gq((unsigned)doc_tiles_most(s.n_docs, s.q_tokens, 64), s.n_heads), gk((unsigned)doc_tiles_most(s.n_docs, s.k_tokens, 64), s.n_kv_heads);
+  attn_form(s, [&](auto Tc, auto Dc) {
+    using T = decltype(Tc);
+    constexpr int DH = decltype(Dc)::value;
+    if (s.q_tokens > 0) hipLaunchKernelGGL((packed_attention_dq_kernel<T, DH>), gq, dim3(256), 0, st, a);
+    if (s.k_tokens > 0) hipLaunchKernelGGL((packed_attention_dkv_kernel<T, DH>), gk, dim3(256), 0, st, a);
+  });
+  BR_LAUNCH_CHECK();
+  return BR_OK;
+}
+
+}  // namespace br
