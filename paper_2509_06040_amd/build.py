@@ -14,7 +14,7 @@ LIB = os.path.join(HERE, "libbranchrollout.so")
 SOURCES = ["tree.cpp", "sde_kernels.hip", "tree_kernels.hip", "dit_kernels.hip", "gemm_bf16.hip", "gemm_bf16_stream.hip", "gemm_bf16_ring.hip", "gemm_small.hip", "gemm_f32.hip", "gemm_f32_ring.hip", "block_rows.hip",
            "attn_bf16.hip", "attn_f32.hip",
            "forward.hip", "api.hip", "ops_api.hip", "prof.cpp",
-           "attn_train.hip", "norm_train.hip", "objective_grad.hip", "adamw.hip", "train_api.hip"]
+           "attn_train.hip", "attn_packed_bf16.hip", "norm_train.hip", "objective_grad.hip", "adamw.hip", "train_api.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 

@@ -4,18 +4,9 @@
 // that the workgroup stages in LDS.  Scores are taken so that a lane holds four rows of the tile for ONE row of its own per block of 16 (C layout of the 16x16
 // matrix instructions); exponentiated, these registers are, without moving, the column operand of the products that contract over the tile's rows, whose row
 // operand is read from LDS transposed.
-#include "dit.h"
-#include "docs.h"
-#include "train.h"
+#include "attn_packed.h"
 
 namespace br {
-
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-
-constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 // Operands of a type.  A fragment holds EPL consecutive contraction indices of quarter g of the lanes: a step contracts 4 EPL of them.
 template <typename T>
@@ -103,30 +94,6 @@ static __device__ inline typename Op<T>::Frag step_of(const f32x4 (&p)[4], int k
   }
 }
 
-__device__ inline float quarters_max(float x) {
-  x = __builtin_elementwise_maximum(x, __shfl_xor(x, 16, 64));
-  return __builtin_elementwise_maximum(x, __shfl_xor(x, 32, 64));
-}
-__device__ inline float quarters_sum(float x) {
-  x += __shfl_xor(x, 16, 64);
-  return x + __shfl_xor(x, 32, 64);
-}
-
-struct AttnArgs {
-  br_attn_shape s;
-  float scale;
-  const void *q, *k, *v, *out, *dout;
-  float *lse, *delta;
-  void *o, *dq, *dk, *dv;
-};
-
-// The keys of the document with the queries of `span`.
-__device__ inline DocSpan other_rows(const int* off, int n, int rows, const DocSpan& span) {
-  DocSpan o{-1, 0, 0};
-  if (span.doc >= 0) o = doc_item(off, n, rows, span.doc + 1);
-  return o;
-}
-
 template <typename T, int DH>
 __global__ __launch_bounds__(256) void packed_attention_kernel(AttnArgs a) {
   using O = Op<T>;
@@ -134,10 +101,10 @@ __global__ __launch_bounds__(256) void packed_attention_kernel(AttnArgs a) {
   constexpr int KS = DH / (4 * O::EPL), PS = TILE_ROWS / (4 * O::EPL), DB = DH / 16;
   __shared__ __attribute__((aligned(16))) char lds[2 * L::BYTES];
   DocSpan span;
-  int first;
-  if (!doc_tile(a.s.q_off, a.s.n_docs, a.s.q_tokens, 64, blockIdx.x, &span, &first)) return;
+  int first, head, tile;
+  if (!head_tile(a.s.n_heads, a.tiles, &head, &tile) || !doc_tile(a.s.q_off, a.s.n_docs, a.s.q_tokens, 64, tile, &span, &first)) return;
   const DocSpan keys = other_rows(a.s.k_off, a.s.n_docs, a.s.k_tokens, span);
-  const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4, head = blockIdx.y, kv = head / (a.s.n_heads / a.s.n_kv_heads);
+  const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4, kv = head / (a.s.n_heads / a.s.n_kv_heads);
   const int row = first + (threadIdx.x >> 6) * 16 + l16;
   const T *k = (const T*)a.k + (size_t)kv * DH, *v = (const T*)a.v + (size_t)kv * DH;
   typename O::Frag q[KS];
@@ -195,7 +162,7 @@ __global__ __launch_bounds__(256) void packed_attention_kernel(AttnArgs a) {
   if (g == 0) a.lse[(size_t)head * a.s.q_tokens + row] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * LN2;
 }
 
-// dq, and delta_i = dout_i . out_i for the kernel of dk and dv.
+// dq, and ref and delta for the kernel of dk and dv.
 template <typename T, int DH>
 __global__ __launch_bounds__(256) void packed_attention_dq_kernel(AttnArgs a) {
   using O = Op<T>;
@@ -203,10 +170,10 @@ __global__ __launch_bounds__(256) void packed_attention_dq_kernel(AttnArgs a) {
   constexpr int KS = DH / (4 * O::EPL), PS = TILE_ROWS / (4 * O::EPL), DB = DH / 16;
   __shared__ __attribute__((aligned(16))) char lds[2 * L::BYTES];
   DocSpan span;
-  int first;
-  if (!doc_tile(a.s.q_off, a.s.n_docs, a.s.q_tokens, 64, blockIdx.x, &span, &first)) return;
+  int first, head, tile;
+  if (!head_tile(a.s.n_heads, a.tiles, &head, &tile) || !doc_tile(a.s.q_off, a.s.n_docs, a.s.q_tokens, 64, tile, &span, &first)) return;
   const DocSpan keys = other_rows(a.s.k_off, a.s.n_docs, a.s.k_tokens, span);
-  const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4, head = blockIdx.y, kv = head / (a.s.n_heads / a.s.n_kv_heads);
+  const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4, kv = head / (a.s.n_heads / a.s.n_kv_heads);
   const int row = first + (threadIdx.x >> 6) * 16 + l16;
   const T *k = (const T*)a.k + (size_t)kv * DH, *v = (const T*)a.v + (size_t)kv * DH;
   typename O::Frag q[KS], dout[KS];
@@ -223,9 +190,12 @@ __global__ __launch_bounds__(256) void packed_attention_dq_kernel(AttnArgs a) {
     delta = quarters_sum(delta);
     if (row < span.end) {
       const size_t at = (size_t)head * a.s.q_tokens + row;
-      if (g == 0) a.delta[at] = delta;
       const float lse = a.lse[at];
       if (lse != -INFINITY) ref = lse * LOG2E;
+      if (g == 0) {
+        a.ref[at] = ref;
+        a.delta[at] = delta;
+      }
     }
   }
   f32x4 dq[DB];
@@ -274,10 +244,10 @@ __global__ __launch_bounds__(256) void packed_attention_dkv_kernel(AttnArgs a) {
   __shared__ __attribute__((aligned(16))) char lds[2 * L::BYTES];
   __shared__ __attribute__((aligned(16))) float refs[2 * TILE_ROWS];  // lse in powers of two (infinite where there is no query), delta
   DocSpan span;
-  int first;
-  if (!doc_tile(a.s.k_off, a.s.n_docs, a.s.k_tokens, 64, blockIdx.x, &span, &first)) return;
+  int first, kv, tile;
+  if (!head_tile(a.s.n_kv_heads, a.tiles, &kv, &tile) || !doc_tile(a.s.k_off, a.s.n_docs, a.s.k_tokens, 64, tile, &span, &first)) return;
   const DocSpan queries = other_rows(a.s.q_off, a.s.n_docs, a.s.q_tokens, span);
-  const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4, kv = blockIdx.y, share = a.s.n_heads / a.s.n_kv_heads;
+  const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4, share = a.s.n_heads / a.s.n_kv_heads;
   const int row = first + (threadIdx.x >> 6) * 16 + l16;
   typename O::Frag k[KS], v[KS];
   own_rows<T, DH>(k, (const T*)a.k + (size_t)kv * DH, a.s.k_stride, row, span.end);
@@ -295,8 +265,7 @@ __global__ __launch_bounds__(256) void packed_attention_dkv_kernel(AttnArgs a) {
       if (threadIdx.x < TILE_ROWS) {
         const int i = q0 + threadIdx.x;
         const size_t at = (size_t)head * a.s.q_tokens + i;
-        const float lse = i < queries.end ? a.lse[at] : -INFINITY;
-        refs[threadIdx.x] = lse == -INFINITY ? INFINITY : lse * LOG2E;
+        refs[threadIdx.x] = i < queries.end ? a.ref[at] : INFINITY;
         refs[TILE_ROWS + threadIdx.x] = i < queries.end ? a.delta[at] : 0.f;
       }
       __syncthreads();
@@ -360,7 +329,7 @@ static void attn_form(const br_attn_shape& s, F f) {
 #undef BR_D
 }
 
-size_t attn_train_workspace(const br_attn_shape& s, bool backward) { return backward ? align_up((size_t)s.n_heads * s.q_tokens * 4, 256) : 0; }
+size_t attn_train_workspace(const br_attn_shape& s, bool backward) { return backward ? 2 * align_up((size_t)s.n_heads * s.q_tokens * 4, 256) : 0; }
 
 br_status launch_attn_train_forward(const br_attn_shape& s, const void* q, const void* k, const void* v, void* out, float* lse, void* ws, hipStream_t st) {
   AttnArgs a = attn_args(s);
@@ -369,8 +338,10 @@ br_status launch_attn_train_forward(const br_attn_shape& s, const void* q, const
   a.v = v;
   a.o = out;
   a.lse = lse;
-  const dim3 grid((unsigned)doc_tiles_most(s.n_docs, s.q_tokens, 64), s.n_heads);
-  attn_form(s, [&](auto Tc, auto Dc) { hipLaunchKernelGGL((packed_attention_kernel<decltype(Tc), decltype(Dc)::value>), grid, dim3(256), 0, st, a); });
+  a.tiles = (int)doc_tiles_most(s.n_docs, s.q_tokens, 64);
+  const long long blocks = head_tile_blocks(s.n_heads, a.tiles);
+  BR_REQUIRE(blocks < 0x7FFFFFFFLL, BR_ESHAPE, "br_attention_forward: too many workgroups for one launch");
+  attn_form(s, [&](auto Tc, auto Dc) { hipLaunchKernelGGL((packed_attention_kernel<decltype(Tc), decltype(Dc)::value>), dim3((unsigned)blocks), dim3(256), 0, st, a); });
   BR_LAUNCH_CHECK();
   return BR_OK;
 }
@@ -384,16 +355,22 @@ br_status launch_attn_train_backward(const br_attn_shape& s, const void* dout, c
   a.out = out;
   a.dout = dout;
   a.lse = const_cast<float*>(lse);
-  a.delta = reinterpret_cast<float*>(ws);
+  a.ref = reinterpret_cast<float*>(ws);
+  a.delta = reinterpret_cast<float*>(reinterpret_cast<char*>(ws) + align_up((size_t)s.n_heads * s.q_tokens * 4, 256));
   a.dq = dq;
   a.dk = dk;
   a.dv = dv;
-  const dim3 gq((unsigned)doc_tiles_most(s.n_docs, s.q_tokens, 64), s.n_heads), gk((unsigned)doc_tiles_most(s.n_docs, s.k_tokens, 64), s.n_kv_heads);
+  const int tq = (int)doc_tiles_most(s.n_docs, s.q_tokens, 64), tk = (int)doc_tiles_most(s.n_docs, s.k_tokens, 64);
+  const long long bq = head_tile_blocks(s.n_heads, tq), bk = head_tile_blocks(s.n_kv_heads, tk);
+  BR_REQUIRE(bq < 0x7FFFFFFFLL && bk < 0x7FFFFFFFLL, BR_ESHAPE, "br_attention_backward: too many workgroups for one launch");
+  if (attn_grad_bf16_fits(s)) return launch_attn_grad_bf16(a, st);
   attn_form(s, [&](auto Tc, auto Dc) {
     using T = decltype(Tc);
     constexpr int DH = decltype(Dc)::value;
-    if (s.q_tokens > 0) hipLaunchKernelGGL((packed_attention_dq_kernel<T, DH>), gq, dim3(256), 0, st, a);
-    if (s.k_tokens > 0) hipLaunchKernelGGL((packed_attention_dkv_kernel<T, DH>), gk, dim3(256), 0, st, a);
+    a.tiles = tq;
+    if (s.q_tokens > 0) hipLaunchKernelGGL((packed_attention_dq_kernel<T, DH>), dim3((unsigned)bq), dim3(256), 0, st, a);
+    a.tiles = tk;
+    if (s.k_tokens > 0) hipLaunchKernelGGL((packed_attention_dkv_kernel<T, DH>), dim3((unsigned)bk), dim3(256), 0, st, a);
   });
   BR_LAUNCH_CHECK();
   return BR_OK;
