@@ -54,7 +54,8 @@ __device__ inline bool head_tile(int heads, int tiles, int* head, int* tile) {
 }
 
 // ---- attn_packed_bf16.hip
-bool attn_grad_bf16_fits(const br_attn_shape& s);
+bool attn_packed_bf16_fits(const br_attn_shape& s);
+br_status launch_attn_forward_bf16(AttnArgs a, hipStream_t st);
 br_status launch_attn_grad_bf16(AttnArgs a, hipStream_t st);
 
 }  // namespace br

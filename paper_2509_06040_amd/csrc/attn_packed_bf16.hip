@@ -1,7 +1,7 @@
-// The backward pass of bf16 attention over packed documents: dq (own rows: queries, tiles of keys), and dk with dv (own rows: keys, tiles of queries).
+// bf16 attention over packed documents: the forward pass, dq (own rows: queries, tiles of keys), and dk with dv (own rows: keys, tiles of queries).
 //
-// A wavefront keeps 32 rows of its side in registers (column operands of both score products) and their gradients in accumulators, and walks tiles of 32
-// rows of the other side in LDS.  Tile j: scores S = Y1 X1 and X = Y2 X2 (X1, X2: own q and dout, or own k and v), probabilities P = exp2(S - ref), dS = P
+// A wavefront keeps 32 rows of its side in registers (column operands of the score products) and their sums in accumulators, and walks tiles of 32
+// rows of the other side in LDS.  Tile j of the backward pass: scores S = Y1 X1 and X = Y2 X2 (X1, X2: own q and dout, or own k and v), probabilities P = exp2(S - ref), dS = P
 // (X - delta), and the products with the tile's rows, dk += Y1^T dS (dq the same) and dv += Y2^T P.  These wait for the next tile: between its scores' last
 // matrix instructions and theirs stand the exponentials of the tile itself.
 //
@@ -14,9 +14,9 @@ namespace br {
 
 #define BR_LPTR(p) ((void __attribute__((address_space(3)))*)(p))
 
-extern __shared__ __attribute__((aligned(1024))) char g_grad_tiles[];
+extern __shared__ __attribute__((aligned(1024))) char g_packed_tiles[];
 
-constexpr int GRAD_TILE = 32, GRAD_NB = 4, GRAD_OWN = 128;  // rows of a tile, buffers, own rows of a workgroup
+constexpr int PACK_TILE = 32, PACK_NB = 4, PACK_OWN = 128;  // rows of a tile, buffers, own rows of a workgroup
 
 static __device__ inline u32x4 buffer_rows(const void* p, unsigned bytes) {
   const unsigned long long v = reinterpret_cast<unsigned long long>(p);
@@ -24,25 +24,294 @@ static __device__ inline u32x4 buffer_rows(const void* p, unsigned bytes) {
                (unsigned)__builtin_amdgcn_readfirstlane(bytes), 0x00020000u};
 }
 
+// Slot permutation of a tile's rows: 16-byte chunk c of row r sits in slot c ^ tile_swz(r).
 template <int DH>
-constexpr int GRAD_LDS = GRAD_NB * (2 * GRAD_TILE * DH * 2 + 2 * GRAD_TILE * 4);
+__device__ inline int tile_swz(int r) { return DH == 128 ? ((r & 7) << 1 | (r >> 3 & 1)) : ((r >> 1 & 3) << 1 | (r >> 3 & 1)); }
+
+// Two matrices' rows on their way into LDS in tiles of PACK_TILE rows, those of the second behind those of the first: 1 KB an instruction, lane i fills bytes
+// 16 i .. 16 i + 15, so the permutation is applied on the global side; rows past the document's end lie past the buffer's and arrive as zeros.
+template <int DH>
+struct TilePair {
+  static constexpr int CH = DH / 8, RPI = 64 / CH, LPW = PACK_TILE / RPI / 4, ROW_B = DH * 2, TILE_B = PACK_TILE * ROW_B, BUF_B = 2 * TILE_B;
+  static_assert(LPW >= 1, "");
+  u32x4 rows1, rows2;
+  unsigned lb1, lb2, off1[LPW], off2[LPW], lds_w;
+  int n_rows;
+  // `heads` heads of DH values side by side, from y1 and y2 on
+  __device__ __forceinline__ void open(const bf16* y1, long long ld1, const bf16* y2, long long ld2, int n, int heads, const char* lds, int wv) {
+    n_rows = n;
+    lb1 = (unsigned)(ld1 * 2);
+    lb2 = (unsigned)(ld2 * 2);
+    rows1 = buffer_rows(y1, (unsigned)(n - 1) * lb1 + heads * ROW_B);
+    rows2 = buffer_rows(y2, (unsigned)(n - 1) * lb2 + heads * ROW_B);
+    lds_w = (unsigned)(uintptr_t)BR_LPTR(const_cast<char*>(lds)) + wv * LPW * 1024;
+    rewind(0, wv);
+  }
+  __device__ __forceinline__ void rewind(int head, int wv) {  // to the first tile of a head
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int t = 0; t < LPW; ++t) {
+      const int r = (wv * LPW + t) * RPI + lane / CH;
+      const unsigned c = head * ROW_B + ((lane % CH ^ tile_swz<DH>(r)) << 4);
+      off1[t] = r < n_rows ? r * lb1 + c : 0xFFFFFFFFu;
+      off2[t] = r < n_rows ? r * lb2 + c : 0xFFFFFFFFu;
+    }
+  }
+  __device__ __forceinline__ void next(int buf) {  // this wave's share of the next tile, into the buffer `buf` bytes on
+#pragma unroll
+    for (int t = 0; t < LPW; ++t) {
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds_w + buf + t * 1024), "v"(off1[t]), "s"(rows1) : "memory", "m0");
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds_w + buf + TILE_B + t * 1024), "v"(off2[t]), "s"(rows2) : "memory", "m0");
+      off1[t] = __builtin_elementwise_add_sat(off1[t], PACK_TILE * lb1);
+      off2[t] = __builtin_elementwise_add_sat(off2[t], PACK_TILE * lb2);
+    }
+  }
+};
+
+// This lane's fragments of a tile: 16 rows from 16 blk on (row operand, channels of step ks), or 16 channels (row operand transposed, all 32 rows: slot (quarter g, e) of
+// the contraction is row 16 (e / 4) + 4 g + e % 4).
+template <int DH>
+struct TileFrags {
+  static constexpr int KS = DH / 32, DB = DH / 16, ROW_B = DH * 2;
+  typedef const char __attribute__((address_space(3)))* lptr;
+  lptr l0;
+  unsigned raddr[KS], caddr[DB];
+  __device__ __forceinline__ void open(const char* lds) {
+    const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4, crow = 4 * g + (l16 >> 2);
+    l0 = (lptr)BR_LPTR(const_cast<char*>(lds));
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) raddr[ks] = l16 * ROW_B + (((ks * 4 + g) ^ tile_swz<DH>(l16)) << 4);
+#pragma unroll
+    for (int d = 0; d < DB; ++d) caddr[d] = crow * ROW_B + (((2 * d + ((l16 & 3) >> 1)) ^ tile_swz<DH>(crow)) << 4) + 8 * (l16 & 1);
+  }
+  __device__ __forceinline__ bf16x8 rows(int blk, int ks, int at) const { return *(const bf16x8 __attribute__((address_space(3)))*)(l0 + raddr[ks] + (at + blk * 16 * ROW_B)); }
+  __device__ __forceinline__ bf16x8 cols(int d, int at) const {
+    const lptr p = l0 + caddr[d] + at;
+    union { s16x4 s[2]; bf16x8 v; } u;
+    u.s[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)p);
+    u.s[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(p + 16 * ROW_B));
+    return u.v;
+  }
+};
+
+__device__ __forceinline__ f32x4 mma(bf16x8 x, bf16x8 y, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, c, 0, 0, 0); }
+
+// Behind step j: tile j + 2 has landed, every wave is done with tile j - 1, whose buffer takes tile j + 3.
+__device__ __forceinline__ void tile_turn() {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// What tile -1 is read as in the first step: finite, with operands of zero beside it.
+template <int DH>
+static __device__ __forceinline__ void clear_last_buffer(char* lds) {
+  constexpr int BUF_B = TilePair<DH>::BUF_B;
+  for (int at = threadIdx.x * 16; at < BUF_B; at += 256 * 16) *reinterpret_cast<u32x4*>(lds + (PACK_NB - 1) * BUF_B + at) = u32x4{0, 0, 0, 0};
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+}
+
+constexpr float REF_LIMIT = 2048.f;  // a query's reference moves when eight of its probabilities add up to more
+
+template <int DH>
+constexpr int FORWARD_LDS = PACK_NB * TilePair<DH>::BUF_B;
+
+// Output and log-sum-exp of 128 queries.  Which reference is subtracted from the scores of a query does not matter, as long as it is the same for all it
+// sums: it is the maximum of some tile, and moves only when a lane's eight probabilities of a tile add up to more than REF_LIMIT, so that no maximum is taken
+// on the way.
+template <int DH>
+__global__ __launch_bounds__(256, DH == 128 ? 2 : 3) void packed_forward_bf16_kernel(AttnArgs a) {
+  using TP = TilePair<DH>;
+  constexpr int KS = DH / 32, DB = DH / 16, BUF_B = TP::BUF_B, TILE_B = TP::TILE_B, QB = 2;
+  constexpr int NA = 2 * KS, NC = DB, NS = NA + NC, FR = 4, RA = FR - 1;
+  static_assert(NS % FR == 0, "");
+  char* lds = g_packed_tiles;
+  const int share = a.s.n_heads / a.s.n_kv_heads;
+  int head, tile, own0;
+  DocSpan own;
+  if (!head_tile(a.s.n_heads, a.tiles, &head, &tile) || !doc_tile(a.s.q_off, a.s.n_docs, a.s.q_tokens, PACK_OWN, tile, &own, &own0)) return;
+  const DocSpan keys = other_rows(a.s.k_off, a.s.n_docs, a.s.k_tokens, own);
+  const int kv = head / share, lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4;
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row0 = own0 + wv * 32;
+  const bool active = row0 < own.end;  // (uniform over the wave)
+  const int n_keys = keys.end - keys.first, N = (n_keys + PACK_TILE - 1) / PACK_TILE;
+
+  bf16x8 q[QB][KS];
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+      q[qb][ks] = *reinterpret_cast<const bf16x8*>((const bf16*)a.q + (size_t)min(row0 + qb * 16 + l16, own.end - 1) * a.s.q_stride + (size_t)head * DH + ks * 32 + g * 8);
+  f32x4 o[DB][QB];
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) o[d][qb] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float ref[QB], sum[QB];  // reference, in powers of two; sum of this lane's probabilities
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    ref[qb] = -3.4028235e38f;  // (the first score above -inf moves it)
+    sum[qb] = 0.f;
+  }
+  if (N > 0) {
+    TP tiles;
+    tiles.open((const bf16*)a.k + (size_t)kv * DH + (size_t)keys.first * a.s.k_stride, a.s.k_stride, (const bf16*)a.v + (size_t)kv * DH + (size_t)keys.first * a.s.v_stride, a.s.v_stride,
+               n_keys, 1, lds, wv);
+    int asked = 0;
+    auto issue = [&](int b) __attribute__((always_inline)) {
+      if (asked < N) tiles.next(b * BUF_B);
+      ++asked;
+    };
+    issue(0);
+    issue(1);
+    issue(2);
+    clear_last_buffer<DH>(lds);
+    tile_turn();
+    if (!active) {  // a wave without rows only keeps up its share of the tile traffic
+      for (int j = 0; j + 1 < N; ++j) {
+        tile_turn();
+        issue((j + 3) % PACK_NB);
+      }
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      return;
+    }
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(q[qb][ks]));
+    TileFrags<DH> frags;
+    frags.open(lds);
+    auto frag_of = [&](auto Nc, int ao, int co) __attribute__((always_inline)) {  // n < NA: scores (block of 16 keys, step of the channels), else values
+      constexpr int n = decltype(Nc)::value;
+      if constexpr (n < NA) return frags.rows(n / KS, n % KS, ao);
+      else return frags.cols(n - NA, co + TILE_B);
+    };
+    const float unit = a.scale * LOG2E;
+    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+    f32x4 s[2][QB];      // [block of 16 keys][block of queries]
+    bf16x8 pf[2][QB];    // [parity of the tile][block of queries]
+    float part[QB];      // sum of this lane's probabilities of the tile
+    bf16x8 fr[FR];
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) pf[1][qb][e] = (bf16)0.f;  // (tile -1)
+    auto use = [&](auto Nc, auto Pc, auto QBc, const bf16x8& f) __attribute__((always_inline)) {  // Pc: parity of the values' tile
+      constexpr int n = decltype(Nc)::value, P = decltype(Pc)::value, qb = decltype(QBc)::value;
+      if constexpr (n < NA) s[n / KS][qb] = mma(f, q[qb][n % KS], n % KS == 0 ? zero : s[n / KS][qb]);
+      else o[n - NA][qb] = mma(f, pf[P][qb], o[n - NA][qb]);
+    };
+    auto prob = [&](auto Pc, int e) __attribute__((always_inline)) {  // element e: block of keys, block of queries, key
+      constexpr int P = decltype(Pc)::value;
+      const int b = e / (4 * QB), qb = (e >> 2) % QB, r = e & 3;
+      const float p = __builtin_amdgcn_exp2f(fmaf(s[b][qb][r], unit, -ref[qb]));
+      part[qb] = b == 0 && r == 0 ? p : part[qb] + p;
+      pf[P][qb][b * 4 + r] = (bf16)p;
+    };
+    auto step = [&](auto Pc, auto Bc, int j) __attribute__((always_inline)) {
+      constexpr int P = decltype(Pc)::value, B = decltype(Bc)::value, BP = (B + PACK_NB - 1) % PACK_NB, BN = (B + 1) % PACK_NB;
+      constexpr int NE = 8 * QB;
+      const bool tail = j == N - 1 && n_keys % PACK_TILE != 0;
+      static_for<NS>([&](auto Nc) __attribute__((always_inline)) {
+        constexpr int n = decltype(Nc)::value;
+        if constexpr (n + RA < NS) fr[(n + RA) % FR] = frag_of(std::integral_constant<int, n + RA>{}, B * BUF_B, BP * BUF_B);
+        else fr[(n + RA) % FR] = frag_of(std::integral_constant<int, n + RA - NS>{}, BN * BUF_B, B * BUF_B);
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (n == NA) {
+          if (tail) {  // keys past the end
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+              for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                  if (j * PACK_TILE + b * 16 + 4 * g + r >= n_keys) s[b][qb][r] = -INFINITY;
+          }
+        }
+        static_for<QB>([&](auto Qc) __attribute__((always_inline)) {
+          use(Nc, std::integral_constant<int, P ^ 1>{}, Qc, fr[n % FR]);
+          __builtin_amdgcn_sched_barrier(0);
+          if constexpr (decltype(Qc)::value == 0 && n >= NA) {
+#pragma unroll
+            for (int e = NE * (n - NA) / NC; e < NE * (n - NA + 1) / NC; ++e) prob(Pc, e);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        });
+      });
+      // (each query moves for itself: its result does not depend on which queries share its wave; a score that is not a number makes its own sum one)
+      if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(part[0] <= REF_LIMIT && part[1] <= REF_LIMIT)) != 0, 0)) {
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) {
+          const bool over = quarters_max(part[qb] <= REF_LIMIT ? 0.f : 1.f) != 0.f;
+          const f32x4 m = __builtin_elementwise_maximum(s[0][qb], s[1][qb]);
+          const float most = quarters_max(__builtin_elementwise_maximum(__builtin_elementwise_maximum(m[0], m[1]), __builtin_elementwise_maximum(m[2], m[3])));
+          const float next = over ? __builtin_elementwise_maximum(ref[qb], most * unit) : ref[qb], shrink = __builtin_amdgcn_exp2f(ref[qb] - next);
+          ref[qb] = next;
+          sum[qb] *= shrink;
+#pragma unroll
+          for (int d = 0; d < DB; ++d) o[d][qb] *= shrink;
+        }
+#pragma unroll
+        for (int e = 0; e < NE; ++e) prob(Pc, e);
+      }
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) sum[qb] += part[qb];
+    };
+    static_for<RA>([&](auto Nc) __attribute__((always_inline)) { fr[decltype(Nc)::value] = frag_of(Nc, 0, 0); });
+    int j = 0;
+    bool more = true;
+    while (more) {
+      static_for<PACK_NB>([&](auto Bc) __attribute__((always_inline)) {
+        if (!more) return;
+        constexpr int B = decltype(Bc)::value, P = B & 1;
+        step(std::integral_constant<int, P>{}, Bc, j);
+        more = ++j < N;
+        if (more) {
+          tile_turn();
+          issue((B + 3) % PACK_NB);
+        } else {  // values of the last tile
+          static_for<NC>([&](auto Ic) __attribute__((always_inline)) {
+            using Nc = std::integral_constant<int, NA + decltype(Ic)::value>;
+            const bf16x8 f = frag_of(Nc{}, 0, B * BUF_B);
+            static_for<QB>([&](auto Qc) __attribute__((always_inline)) { use(Nc{}, std::integral_constant<int, P>{}, Qc, f); });
+          });
+        }
+      });
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  }
+  if (!active) return;
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    const float total = quarters_sum(sum[qb]), inv = total == 0.f ? 0.f : 1.f / total;
+    const int row = row0 + qb * 16 + l16;
+    if (row >= own.end) continue;
+    bf16* out = (bf16*)a.o + (size_t)row * a.s.o_stride + (size_t)head * DH + 4 * g;
+#pragma unroll
+    for (int d = 0; d < DB; ++d) store4(out + 16 * d, o[d][qb][0] * inv, o[d][qb][1] * inv, o[d][qb][2] * inv, o[d][qb][3] * inv);
+    if (g == 0) a.lse[(size_t)head * a.s.q_tokens + row] = total == 0.f ? -INFINITY : (ref[qb] + __builtin_amdgcn_logf(total)) * LN2;
+  }
+}
+
+template <int DH>
+constexpr int GRAD_LDS = PACK_NB * (TilePair<DH>::BUF_B + 2 * PACK_TILE * 4);
 
 // Waves a SIMD: dk and dv of head dim 128 have 128 accumulators and 64 operands a lane.
 template <int DH, bool KEYS>
 __global__ __launch_bounds__(256, DH == 128 && KEYS ? 1 : 2) void packed_grad_bf16_kernel(AttnArgs a) {
-  constexpr int CH = DH / 8, KS = DH / 32, DB = DH / 16, RPI = 64 / CH, LPW = GRAD_TILE / RPI / 4;
-  constexpr int ROW_B = DH * 2, TILE_B = GRAD_TILE * ROW_B, BUF_B = 2 * TILE_B, QB = 2;
+  using TP = TilePair<DH>;
+  constexpr int KS = DH / 32, DB = DH / 16, BUF_B = TP::BUF_B, TILE_B = TP::TILE_B, QB = 2;
   constexpr int NA = 4 * KS, NC = KEYS ? 2 * DB : DB, NS = NA + NC, FR = DH == 128 && KEYS ? 8 : 4, RA = FR - 1;
-  constexpr int REFS = GRAD_NB * BUF_B, REF_B = 2 * GRAD_TILE * 4;  // ref and delta of a tile's rows, behind the tiles
-  static_assert(NS % FR == 0 && LPW >= 1, "");
-  char* lds = g_grad_tiles;
+  constexpr int REFS = PACK_NB * BUF_B, REF_B = 2 * PACK_TILE * 4;  // ref and delta of a tile's rows, behind the tiles
+  static_assert(NS % FR == 0, "");
+  char* lds = g_packed_tiles;
 
   const int share = a.s.n_heads / a.s.n_kv_heads;
   int head, tile, own0;
   DocSpan own;
   const int* own_off = KEYS ? a.s.k_off : a.s.q_off;
   if (!head_tile(KEYS ? a.s.n_kv_heads : a.s.n_heads, a.tiles, &head, &tile) ||
-      !doc_tile(own_off, a.s.n_docs, KEYS ? a.s.k_tokens : a.s.q_tokens, GRAD_OWN, tile, &own, &own0))
+      !doc_tile(own_off, a.s.n_docs, KEYS ? a.s.k_tokens : a.s.q_tokens, PACK_OWN, tile, &own, &own0))
     return;
   const DocSpan other = other_rows(KEYS ? a.s.q_off : a.s.k_off, a.s.n_docs, KEYS ? a.s.q_tokens : a.s.k_tokens, own);
   const int kv = KEYS ? head : head / share, h0 = KEYS ? head * share : head;
@@ -92,72 +361,41 @@ __global__ __launch_bounds__(256, DH == 128 && KEYS ? 1 : 2) void packed_grad_bf
       if constexpr (KEYS) acc2[d][qb] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
-  const int n_rows = other.end - other.first, nt = (n_rows + GRAD_TILE - 1) / GRAD_TILE, N = KEYS ? nt * share : nt;
+  const int n_rows = other.end - other.first, nt = (n_rows + PACK_TILE - 1) / PACK_TILE, N = KEYS ? nt * share : nt;
   if (N > 0) {
-    // ---- tiles: 1 KB an instruction, lane i fills bytes 16 i .. 16 i + 15, so the permutation is applied on the global side; rows past the document's end
-    // lie past the buffer's and arrive as zeros
-    const bf16* y1 = (KEYS ? (const bf16*)a.q + (size_t)h0 * DH : (const bf16*)a.k + (size_t)kv * DH) + (size_t)other.first * (KEYS ? a.s.q_stride : a.s.k_stride);
-    const bf16* y2 = (KEYS ? (const bf16*)a.dout + (size_t)h0 * DH : (const bf16*)a.v + (size_t)kv * DH) + (size_t)other.first * (KEYS ? a.s.o_stride : a.s.v_stride);
-    const unsigned lb1 = (unsigned)((KEYS ? a.s.q_stride : a.s.k_stride) * 2), lb2 = (unsigned)((KEYS ? a.s.o_stride : a.s.v_stride) * 2);
-    const unsigned width = (KEYS ? share : 1) * ROW_B;
-    const u32x4 rows1 = buffer_rows(y1, (unsigned)(n_rows - 1) * lb1 + width), rows2 = buffer_rows(y2, (unsigned)(n_rows - 1) * lb2 + width);
-    auto swz = [](int r) { return DH == 128 ? ((r & 7) << 1 | (r >> 3 & 1)) : ((r >> 1 & 3) << 1 | (r >> 3 & 1)); };
-    unsigned off1[LPW], off2[LPW];
-    const int lrow = lane / CH, slot = lane % CH;
-    auto rewind = [&](int h) __attribute__((always_inline)) {  // first tile of head h0 + h
-#pragma unroll
-      for (int t = 0; t < LPW; ++t) {
-        const int r = (wv * LPW + t) * RPI + lrow;
-        const unsigned c = h * ROW_B + ((slot ^ swz(r)) << 4);
-        off1[t] = r < n_rows ? r * lb1 + c : 0xFFFFFFFFu;
-        off2[t] = r < n_rows ? r * lb2 + c : 0xFFFFFFFFu;
-      }
-    };
-    rewind(0);
-    const unsigned lds0 = (unsigned)(uintptr_t)BR_LPTR(lds), lds_w = lds0 + wv * LPW * 1024;
+    const long long ld_y1 = KEYS ? a.s.q_stride : a.s.k_stride, ld_y2 = KEYS ? a.s.o_stride : a.s.v_stride;
+    TP tiles;
+    tiles.open((KEYS ? (const bf16*)a.q + (size_t)h0 * DH : (const bf16*)a.k + (size_t)kv * DH) + (size_t)other.first * ld_y1, ld_y1,
+               (KEYS ? (const bf16*)a.dout + (size_t)h0 * DH : (const bf16*)a.v + (size_t)kv * DH) + (size_t)other.first * ld_y2, ld_y2, n_rows, KEYS ? share : 1, lds, wv);
+    const unsigned lds0 = (unsigned)(uintptr_t)BR_LPTR(lds);
     int asked = 0, asked_head = 0, asked_tile = 0;
     auto issue = [&](int b) __attribute__((always_inline)) {  // the next tile into buffer b
       if (asked < N) {
-        const int buf = b * BUF_B;
-#pragma unroll
-        for (int t = 0; t < LPW; ++t) {
-          asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds_w + buf + t * 1024), "v"(off1[t]), "s"(rows1) : "memory", "m0");
-          asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds_w + buf + TILE_B + t * 1024), "v"(off2[t]), "s"(rows2) : "memory", "m0");
-          off1[t] = __builtin_elementwise_add_sat(off1[t], GRAD_TILE * lb1);
-          off2[t] = __builtin_elementwise_add_sat(off2[t], GRAD_TILE * lb2);
-        }
+        tiles.next(b * BUF_B);
         if constexpr (KEYS) {  // ref (wave 0) and delta (wave 1) of the tile's queries
           if (wv < 2) {
             const u32x4 d = buffer_rows((wv == 0 ? a.ref : a.delta) + (size_t)(h0 + asked_head) * a.s.q_tokens + other.first, (unsigned)n_rows * 4);
-            if (lane < GRAD_TILE)
-              asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(lds0 + REFS + b * REF_B + wv * (GRAD_TILE * 4)),
-                           "v"((unsigned)(asked_tile * GRAD_TILE + lane) * 4u), "s"(d) : "memory", "m0");
+            if (lane < PACK_TILE)
+              asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(lds0 + REFS + b * REF_B + wv * (PACK_TILE * 4)),
+                           "v"((unsigned)(asked_tile * PACK_TILE + lane) * 4u), "s"(d) : "memory", "m0");
           }
           if (++asked_tile == nt) {
             asked_tile = 0;
-            rewind(++asked_head);
+            tiles.rewind(++asked_head, wv);
           }
         }
         ++asked;
       }
     };
-    // Behind step j: tile j + 2 has landed, every wave is done with tile j - 1, whose buffer takes tile j + 3.
-    auto turn = [&]() __attribute__((always_inline)) {
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      __builtin_amdgcn_s_barrier();
-      asm volatile("" ::: "memory");
-    };
     issue(0);
     issue(1);
     issue(2);
-    // Tile -1, whose gradients are zeros, lies in the last buffer: finite rows there
-    for (int at = tid * 16; at < BUF_B; at += 256 * 16) *reinterpret_cast<u32x4*>(lds + (GRAD_NB - 1) * BUF_B + at) = u32x4{0, 0, 0, 0};
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    turn();
+    clear_last_buffer<DH>(lds);
+    tile_turn();
     if (!active) {  // a wave without rows only keeps up its share of the tile traffic
       for (int j = 0; j + 1 < N; ++j) {
-        turn();
-        issue((j + 3) % GRAD_NB);
+        tile_turn();
+        issue((j + 3) % PACK_NB);
       }
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       return;
@@ -169,31 +407,13 @@ __global__ __launch_bounds__(256, DH == 128 && KEYS ? 1 : 2) void packed_grad_bf
         asm volatile("" : "+v"(f1[qb][ks]), "+v"(f2[qb][ks]));
       }
 
-    unsigned raddr[KS], caddr[DB];  // this lane's fragments in buffer 0
-    static_for<KS>([&](auto Kc) __attribute__((always_inline)) {
-      constexpr int ks = decltype(Kc)::value;
-      raddr[ks] = l16 * ROW_B + (((ks * 4 + g) ^ swz(l16)) << 4);
-    });
-    const int crow = 4 * g + (l16 >> 2);
-    static_for<DB>([&](auto Dc) __attribute__((always_inline)) {
-      constexpr int d = decltype(Dc)::value;
-      caddr[d] = crow * ROW_B + (((2 * d + ((l16 & 3) >> 1)) ^ swz(crow)) << 4) + 8 * (l16 & 1);
-    });
-    typedef const char __attribute__((address_space(3)))* lptr;
-    const lptr l0 = (lptr)BR_LPTR(lds);
+    TileFrags<DH> frags;
+    frags.open(lds);
     // Slot n of a step: a fragment of the scores (n < NA: block of 16 rows, step of the channels, S or X) or of the products behind them.
     auto frag_of = [&](auto Nc, int ao, int co) __attribute__((always_inline)) {  // ao, co: the buffers
-      constexpr int n = decltype(Nc)::value;
-      if constexpr (n < NA) {
-        return *(const bf16x8 __attribute__((address_space(3)))*)(l0 + raddr[(n >> 1) % KS] + (ao + (n & 1) * TILE_B + n / (2 * KS) * 16 * ROW_B));
-      } else {
-        constexpr int i = n - NA, d = KEYS ? i >> 1 : i, y = KEYS ? 1 - (i & 1) : 0;
-        const lptr p = l0 + caddr[d] + (co + y * TILE_B);
-        union { s16x4 s[2]; bf16x8 v; } u;
-        u.s[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)p);
-        u.s[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(p + 16 * ROW_B));
-        return u.v;
-      }
+      constexpr int n = decltype(Nc)::value, i = n - NA;
+      if constexpr (n < NA) return frags.rows(n / (2 * KS), (n >> 1) % KS, ao + (n & 1) * TILE_B);
+      else return frags.cols(KEYS ? i >> 1 : i, co + (KEYS ? 1 - (i & 1) : 0) * TILE_B);
     };
     f32x4 s[2][2][QB];               // [S | X][block of 16 rows][own block]
     bf16x8 pf[2][QB], df[2][QB];     // [parity of the tile][own block]
@@ -203,7 +423,6 @@ __global__ __launch_bounds__(256, DH == 128 && KEYS ? 1 : 2) void packed_grad_bf
 #pragma unroll
       for (int e = 0; e < 8; ++e) pf[1][qb][e] = df[1][qb][e] = (bf16)0.f;  // (tile -1)
     const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-    auto mma = [](bf16x8 x, bf16x8 y, f32x4 c) __attribute__((always_inline)) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, c, 0, 0, 0); };
     const float unit = a.scale * LOG2E;
     f32x4 rv[2], dl[2];  // ref and delta of the tile's rows (KEYS)
     auto prob = [&](auto Pc, int e) __attribute__((always_inline)) {
@@ -227,14 +446,14 @@ __global__ __launch_bounds__(256, DH == 128 && KEYS ? 1 : 2) void packed_grad_bf
     };
     // Step of tile j (parity P, buffer B): its scores, its probabilities behind the first block's, the products of tile j - 1.
     auto step = [&](auto Pc, auto Bc) __attribute__((always_inline)) {
-      constexpr int P = decltype(Pc)::value, B = decltype(Bc)::value, BP = (B + GRAD_NB - 1) % GRAD_NB, BN = (B + 1) % GRAD_NB;
+      constexpr int P = decltype(Pc)::value, B = decltype(Bc)::value, BP = (B + PACK_NB - 1) % PACK_NB, BN = (B + 1) % PACK_NB;
       constexpr int E0 = NA / 2 + 2, EN = NS - 1, NE = 8 * QB;  // the probabilities are taken in these slots
       constexpr int E1 = NA + 1;                                // those of the second block from here on
       if constexpr (KEYS) {
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
-          rv[b] = *(const f32x4 __attribute__((address_space(3)))*)(l0 + (REFS + B * REF_B + b * 64) + g * 16);
-          dl[b] = *(const f32x4 __attribute__((address_space(3)))*)(l0 + (REFS + B * REF_B + GRAD_TILE * 4 + b * 64) + g * 16);
+          rv[b] = *(const f32x4 __attribute__((address_space(3)))*)(frags.l0 + (REFS + B * REF_B + b * 64) + g * 16);
+          dl[b] = *(const f32x4 __attribute__((address_space(3)))*)(frags.l0 + (REFS + B * REF_B + PACK_TILE * 4 + b * 64) + g * 16);
         }
       }
       static_for<NS>([&](auto Nc) __attribute__((always_inline)) {
@@ -262,7 +481,7 @@ __global__ __launch_bounds__(256, DH == 128 && KEYS ? 1 : 2) void packed_grad_bf
     int j = 0;
     bool more = true;
     while (more) {
-      static_for<GRAD_NB>([&](auto Bc) __attribute__((always_inline)) {
+      static_for<PACK_NB>([&](auto Bc) __attribute__((always_inline)) {
         if (!more) return;
         constexpr int B = decltype(Bc)::value, P = B & 1;
         step(std::integral_constant<int, P>{}, Bc);
@@ -271,12 +490,12 @@ __global__ __launch_bounds__(256, DH == 128 && KEYS ? 1 : 2) void packed_grad_bf
           for (int qb = 0; qb < QB; ++qb)
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-              if (j * GRAD_TILE + (e >> 2) * 16 + 4 * g + (e & 3) >= n_rows) df[P][qb][e] = (bf16)0.f;
+              if (j * PACK_TILE + (e >> 2) * 16 + 4 * g + (e & 3) >= n_rows) df[P][qb][e] = (bf16)0.f;
         }
         more = ++j < N;
         if (more) {
-          turn();
-          issue((B + 3) % GRAD_NB);
+          tile_turn();
+          issue((B + 3) % PACK_NB);
         } else {  // products of the last tile
           static_for<NC>([&](auto Ic) __attribute__((always_inline)) {
             using Nc = std::integral_constant<int, NA + decltype(Ic)::value>;
@@ -305,9 +524,18 @@ __global__ __launch_bounds__(256, DH == 128 && KEYS ? 1 : 2) void packed_grad_bf
 }
 
 // Rows of a document are addressed with 32-bit byte offsets from its first one.
-bool attn_grad_bf16_fits(const br_attn_shape& s) {
+bool attn_packed_bf16_fits(const br_attn_shape& s) {
   auto fits = [](int64_t tokens, int64_t stride) { return tokens * stride * 2 < (1LL << 32); };
   return s.dtype == BR_BF16 && fits(s.q_tokens, s.q_stride) && fits(s.q_tokens, s.o_stride) && fits(s.k_tokens, s.k_stride) && fits(s.k_tokens, s.v_stride);
+}
+
+br_status launch_attn_forward_bf16(AttnArgs a, hipStream_t st) {
+  a.tiles = (int)doc_tiles_most(a.s.n_docs, a.s.q_tokens, PACK_OWN);
+  const dim3 grid((unsigned)head_tile_blocks(a.s.n_heads, a.tiles));
+  if (a.s.head_dim == 64) hipLaunchKernelGGL((packed_forward_bf16_kernel<64>), grid, dim3(256), FORWARD_LDS<64>, st, a);
+  else hipLaunchKernelGGL((packed_forward_bf16_kernel<128>), grid, dim3(256), FORWARD_LDS<128>, st, a);
+  BR_LAUNCH_CHECK();
+  return BR_OK;
 }
 
 template <int DH>
@@ -315,7 +543,7 @@ static br_status grad_launch(AttnArgs a, hipStream_t st) {
   auto run = [&](auto KEYSc, int tokens, int heads) -> br_status {
     constexpr bool KEYS = decltype(KEYSc)::value;
     if (tokens == 0) return BR_OK;
-    a.tiles = (int)doc_tiles_most(a.s.n_docs, tokens, GRAD_OWN);
+    a.tiles = (int)doc_tiles_most(a.s.n_docs, tokens, PACK_OWN);
     hipLaunchKernelGGL((packed_grad_bf16_kernel<DH, KEYS>), dim3((unsigned)head_tile_blocks(heads, a.tiles)), dim3(256), GRAD_LDS<DH>, st, a);
     BR_LAUNCH_CHECK();
     return BR_OK;

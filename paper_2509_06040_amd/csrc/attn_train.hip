@@ -341,6 +341,7 @@ br_status launch_attn_train_forward(const br_attn_shape& s, const void* q, const
   a.tiles = (int)doc_tiles_most(s.n_docs, s.q_tokens, 64);
   const long long blocks = head_tile_blocks(s.n_heads, a.tiles);
   BR_REQUIRE(blocks < 0x7FFFFFFFLL, BR_ESHAPE, "br_attention_forward: too many workgroups for one launch");
+  if (attn_packed_bf16_fits(s)) return launch_attn_forward_bf16(a, st);
   attn_form(s, [&](auto Tc, auto Dc) { hipLaunchKernelGGL((packed_attention_kernel<decltype(Tc), decltype(Dc)::value>), dim3((unsigned)blocks), dim3(256), 0, st, a); });
   BR_LAUNCH_CHECK();
   return BR_OK;
@@ -363,7 +364,7 @@ br_status launch_attn_train_backward(const br_attn_shape& s, const void* dout, c
   const int tq = (int)doc_tiles_most(s.n_docs, s.q_tokens, 64), tk = (int)doc_tiles_most(s.n_docs, s.k_tokens, 64);
   const long long bq = head_tile_blocks(s.n_heads, tq), bk = head_tile_blocks(s.n_kv_heads, tk);
   BR_REQUIRE(bq < 0x7FFFFFFFLL && bk < 0x7FFFFFFFLL, BR_ESHAPE, "br_attention_backward: too many workgroups for one launch");
-  if (attn_grad_bf16_fits(s)) return launch_attn_grad_bf16(a, st);
+  if (attn_packed_bf16_fits(s)) return launch_attn_grad_bf16(a, st);
   attn_form(s, [&](auto Tc, auto Dc) {
     using T = decltype(Tc);
     constexpr int DH = decltype(Dc)::value;
