@@ -5,7 +5,7 @@
 // (X - delta), and the products with the tile's rows, dk += Y1^T dS (dq the same) and dv += Y2^T P.  These wait for the next tile: between its scores' last
 // matrix instructions and theirs stand the exponentials of the tile itself.
 //
-// Tiles come straight from global memory into LDS (four buffers), rows as they lie, 16-byte chunks permuted per row so that both the fragments of 16 rows
+// Tiles come straight from global memory into LDS, rows as they lie, 16-byte chunks permuted per row so that both the fragments of 16 rows
 // and the transposed reads (eight rows, two chunks) spread over the banks.
 #include "attn_packed.h"
 #include "static_for.h"
@@ -16,7 +16,16 @@ namespace br {
 
 extern __shared__ __attribute__((aligned(1024))) char g_packed_tiles[];
 
-constexpr int PACK_TILE = 32, PACK_NB = 4, PACK_OWN = 128;  // rows of a tile, buffers, own rows of a workgroup
+constexpr int PACK_TILE = 32, PACK_OWN = 128;  // rows of a tile, own rows of a workgroup
+
+// Waves a SIMD, buffers, and tiles between two barriers.
+enum class Pass { FORWARD, QUERIES, KEYS };
+template <int DH, Pass PASS>
+struct PackForm {
+  static constexpr int WPE = DH == 128 ? (PASS == Pass::KEYS ? 1 : 2) : PASS == Pass::KEYS ? 2 : 3;
+  static constexpr int NB = DH == 128 ? (PASS == Pass::KEYS ? 6 : 4) : 6, EACH = NB >= 6 ? 2 : 1;
+  static constexpr int LDS = NB * (2 * PACK_TILE * DH * 2 + (PASS == Pass::KEYS ? 2 * PACK_TILE * 4 : 0));
+};
 
 static __device__ inline u32x4 buffer_rows(const void* p, unsigned bytes) {
   const unsigned long long v = reinterpret_cast<unsigned long long>(p);
@@ -96,7 +105,8 @@ struct TileFrags {
 
 __device__ __forceinline__ f32x4 mma(bf16x8 x, bf16x8 y, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, c, 0, 0, 0); }
 
-// Behind step j: tile j + 2 has landed, every wave is done with tile j - 1, whose buffer takes tile j + 3.
+// Behind every EACH-th step j: the tiles asked for at the last turn have landed, every wave is done with those before tile j, whose buffers take the tiles
+// from j + NB - EACH on.
 __device__ __forceinline__ void tile_turn() {
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __builtin_amdgcn_s_barrier();
@@ -104,27 +114,26 @@ __device__ __forceinline__ void tile_turn() {
 }
 
 // What tile -1 is read as in the first step: finite, with operands of zero beside it.
-template <int DH>
+template <int DH, int NB>
 static __device__ __forceinline__ void clear_last_buffer(char* lds) {
   constexpr int BUF_B = TilePair<DH>::BUF_B;
-  for (int at = threadIdx.x * 16; at < BUF_B; at += 256 * 16) *reinterpret_cast<u32x4*>(lds + (PACK_NB - 1) * BUF_B + at) = u32x4{0, 0, 0, 0};
+  for (int at = threadIdx.x * 16; at < BUF_B; at += 256 * 16) *reinterpret_cast<u32x4*>(lds + (NB - 1) * BUF_B + at) = u32x4{0, 0, 0, 0};
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 }
 
 constexpr float REF_LIMIT = 2048.f;  // a query's reference moves when eight of its probabilities add up to more
 
-template <int DH>
-constexpr int FORWARD_LDS = PACK_NB * TilePair<DH>::BUF_B;
-
 // Output and log-sum-exp of 128 queries.  Which reference is subtracted from the scores of a query does not matter, as long as it is the same for all it
 // sums: it is the maximum of some tile, and moves only when a lane's eight probabilities of a tile add up to more than REF_LIMIT, so that no maximum is taken
 // on the way.
 template <int DH>
-__global__ __launch_bounds__(256, DH == 128 ? 2 : 3) void packed_forward_bf16_kernel(AttnArgs a) {
+__global__ __launch_bounds__(256, (PackForm<DH, Pass::FORWARD>::WPE)) void packed_forward_bf16_kernel(AttnArgs a) {
+  using F = PackForm<DH, Pass::FORWARD>;
+  constexpr int NB = F::NB, EACH = F::EACH;
   using TP = TilePair<DH>;
   constexpr int KS = DH / 32, DB = DH / 16, BUF_B = TP::BUF_B, TILE_B = TP::TILE_B, QB = 2;
   constexpr int NA = 2 * KS, NC = DB, NS = NA + NC, FR = 4, RA = FR - 1;
-  static_assert(NS % FR == 0, "");
+  static_assert(NS % FR == 0 && NB % 2 == 0 && NB % EACH == 0 && NB >= 2 + 2 * EACH, "");
   char* lds = g_packed_tiles;
   const int share = a.s.n_heads / a.s.n_kv_heads;
   int head, tile, own0;
@@ -162,15 +171,15 @@ __global__ __launch_bounds__(256, DH == 128 ? 2 : 3) void packed_forward_bf16_ke
       if (asked < N) tiles.next(b * BUF_B);
       ++asked;
     };
-    issue(0);
-    issue(1);
-    issue(2);
-    clear_last_buffer<DH>(lds);
+#pragma unroll
+    for (int b = 0; b + 1 < NB; ++b) issue(b);
+    clear_last_buffer<DH, NB>(lds);
     tile_turn();
     if (!active) {  // a wave without rows only keeps up its share of the tile traffic
-      for (int j = 0; j + 1 < N; ++j) {
+      for (int j = EACH - 1, b = NB - 1; j + 1 < N; j += EACH) {
         tile_turn();
-        issue((j + 3) % PACK_NB);
+#pragma unroll
+        for (int i = 0; i < EACH; ++i, b = b + 1 == NB ? 0 : b + 1) issue(b);
       }
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       return;
@@ -209,7 +218,7 @@ __global__ __launch_bounds__(256, DH == 128 ? 2 : 3) void packed_forward_bf16_ke
       pf[P][qb][b * 4 + r] = (bf16)p;
     };
     auto step = [&](auto Pc, auto Bc, int j) __attribute__((always_inline)) {
-      constexpr int P = decltype(Pc)::value, B = decltype(Bc)::value, BP = (B + PACK_NB - 1) % PACK_NB, BN = (B + 1) % PACK_NB;
+      constexpr int P = decltype(Pc)::value, B = decltype(Bc)::value, BP = (B + NB - 1) % NB, BN = (B + 1) % NB;
       constexpr int NE = 8 * QB;
       const bool tail = j == N - 1 && n_keys % PACK_TILE != 0;
       static_for<NS>([&](auto Nc) __attribute__((always_inline)) {
@@ -261,14 +270,17 @@ __global__ __launch_bounds__(256, DH == 128 ? 2 : 3) void packed_forward_bf16_ke
     int j = 0;
     bool more = true;
     while (more) {
-      static_for<PACK_NB>([&](auto Bc) __attribute__((always_inline)) {
+      static_for<NB>([&](auto Bc) __attribute__((always_inline)) {
         if (!more) return;
         constexpr int B = decltype(Bc)::value, P = B & 1;
         step(std::integral_constant<int, P>{}, Bc, j);
         more = ++j < N;
         if (more) {
-          tile_turn();
-          issue((B + 3) % PACK_NB);
+          if constexpr (B % EACH == EACH - 1) {
+            tile_turn();
+#pragma unroll
+            for (int i = EACH; i > 0; --i) issue((B + NB - i) % NB);
+          }
         } else {  // values of the last tile
           static_for<NC>([&](auto Ic) __attribute__((always_inline)) {
             using Nc = std::integral_constant<int, NA + decltype(Ic)::value>;
@@ -293,17 +305,17 @@ __global__ __launch_bounds__(256, DH == 128 ? 2 : 3) void packed_forward_bf16_ke
   }
 }
 
-template <int DH>
-constexpr int GRAD_LDS = PACK_NB * (TilePair<DH>::BUF_B + 2 * PACK_TILE * 4);
-
-// Waves a SIMD: dk and dv of head dim 128 have 128 accumulators and 64 operands a lane.
-template <int DH, bool KEYS>
-__global__ __launch_bounds__(256, DH == 128 && KEYS ? 1 : 2) void packed_grad_bf16_kernel(AttnArgs a) {
+// (dk and dv of head dim 128: 128 accumulators and 64 operands a lane, one wave a SIMD)
+template <int DH, Pass PASS>
+__global__ __launch_bounds__(256, (PackForm<DH, PASS>::WPE)) void packed_grad_bf16_kernel(AttnArgs a) {
+  using F = PackForm<DH, PASS>;
+  constexpr bool KEYS = PASS == Pass::KEYS;
+  constexpr int NB = F::NB, EACH = F::EACH;
   using TP = TilePair<DH>;
   constexpr int KS = DH / 32, DB = DH / 16, BUF_B = TP::BUF_B, TILE_B = TP::TILE_B, QB = 2;
   constexpr int NA = 4 * KS, NC = KEYS ? 2 * DB : DB, NS = NA + NC, FR = DH == 128 && KEYS ? 8 : 4, RA = FR - 1;
-  constexpr int REFS = PACK_NB * BUF_B, REF_B = 2 * PACK_TILE * 4;  // ref and delta of a tile's rows, behind the tiles
-  static_assert(NS % FR == 0, "");
+  constexpr int REFS = NB * BUF_B, REF_B = 2 * PACK_TILE * 4;  // ref and delta of a tile's rows, behind the tiles
+  static_assert(NS % FR == 0 && NB % 2 == 0 && NB % EACH == 0 && NB >= 2 + 2 * EACH, "");
   char* lds = g_packed_tiles;
 
   const int share = a.s.n_heads / a.s.n_kv_heads;
@@ -387,15 +399,15 @@ __global__ __launch_bounds__(256, DH == 128 && KEYS ? 1 : 2) void packed_grad_bf
         ++asked;
       }
     };
-    issue(0);
-    issue(1);
-    issue(2);
-    clear_last_buffer<DH>(lds);
+#pragma unroll
+    for (int b = 0; b + 1 < NB; ++b) issue(b);
+    clear_last_buffer<DH, NB>(lds);
     tile_turn();
     if (!active) {  // a wave without rows only keeps up its share of the tile traffic
-      for (int j = 0; j + 1 < N; ++j) {
+      for (int j = EACH - 1, b = NB - 1; j + 1 < N; j += EACH) {
         tile_turn();
-        issue((j + 3) % PACK_NB);
+#pragma unroll
+        for (int i = 0; i < EACH; ++i, b = b + 1 == NB ? 0 : b + 1) issue(b);
       }
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       return;
@@ -446,7 +458,7 @@ __global__ __launch_bounds__(256, DH == 128 && KEYS ? 1 : 2) void packed_grad_bf
     };
     // Step of tile j (parity P, buffer B): its scores, its probabilities behind the first block's, the products of tile j - 1.
     auto step = [&](auto Pc, auto Bc) __attribute__((always_inline)) {
-      constexpr int P = decltype(Pc)::value, B = decltype(Bc)::value, BP = (B + PACK_NB - 1) % PACK_NB, BN = (B + 1) % PACK_NB;
+      constexpr int P = decltype(Pc)::value, B = decltype(Bc)::value, BP = (B + NB - 1) % NB, BN = (B + 1) % NB;
       constexpr int E0 = NA / 2 + 2, EN = NS - 1, NE = 8 * QB;  // the probabilities are taken in these slots
       constexpr int E1 = NA + 1;                                // those of the second block from here on
       if constexpr (KEYS) {
@@ -481,7 +493,7 @@ __global__ __launch_bounds__(256, DH == 128 && KEYS ? 1 : 2) void packed_grad_bf
     int j = 0;
     bool more = true;
     while (more) {
-      static_for<PACK_NB>([&](auto Bc) __attribute__((always_inline)) {
+      static_for<NB>([&](auto Bc) __attribute__((always_inline)) {
         if (!more) return;
         constexpr int B = decltype(Bc)::value, P = B & 1;
         step(std::integral_constant<int, P>{}, Bc);
@@ -494,8 +506,11 @@ __global__ __launch_bounds__(256, DH == 128 && KEYS ? 1 : 2) void packed_grad_bf
         }
         more = ++j < N;
         if (more) {
-          tile_turn();
-          issue((B + 3) % PACK_NB);
+          if constexpr (B % EACH == EACH - 1) {
+            tile_turn();
+#pragma unroll
+            for (int i = EACH; i > 0; --i) issue((B + NB - i) % NB);
+          }
         } else {  // products of the last tile
           static_for<NC>([&](auto Ic) __attribute__((always_inline)) {
             using Nc = std::integral_constant<int, NA + decltype(Ic)::value>;
@@ -532,24 +547,25 @@ bool attn_packed_bf16_fits(const br_attn_shape& s) {
 br_status launch_attn_forward_bf16(AttnArgs a, hipStream_t st) {
   a.tiles = (int)doc_tiles_most(a.s.n_docs, a.s.q_tokens, PACK_OWN);
   const dim3 grid((unsigned)head_tile_blocks(a.s.n_heads, a.tiles));
-  if (a.s.head_dim == 64) hipLaunchKernelGGL((packed_forward_bf16_kernel<64>), grid, dim3(256), FORWARD_LDS<64>, st, a);
-  else hipLaunchKernelGGL((packed_forward_bf16_kernel<128>), grid, dim3(256), FORWARD_LDS<128>, st, a);
+  if (a.s.head_dim == 64) hipLaunchKernelGGL((packed_forward_bf16_kernel<64>), grid, dim3(256), (PackForm<64, Pass::FORWARD>::LDS), st, a);
+  else hipLaunchKernelGGL((packed_forward_bf16_kernel<128>), grid, dim3(256), (PackForm<128, Pass::FORWARD>::LDS), st, a);
   BR_LAUNCH_CHECK();
   return BR_OK;
 }
 
 template <int DH>
 static br_status grad_launch(AttnArgs a, hipStream_t st) {
-  auto run = [&](auto KEYSc, int tokens, int heads) -> br_status {
-    constexpr bool KEYS = decltype(KEYSc)::value;
-    if (tokens == 0) return BR_OK;
-    a.tiles = (int)doc_tiles_most(a.s.n_docs, tokens, PACK_OWN);
-    hipLaunchKernelGGL((packed_grad_bf16_kernel<DH, KEYS>), dim3((unsigned)head_tile_blocks(heads, a.tiles)), dim3(256), GRAD_LDS<DH>, st, a);
+  if (a.s.q_tokens > 0) {
+    a.tiles = (int)doc_tiles_most(a.s.n_docs, a.s.q_tokens, PACK_OWN);
+    hipLaunchKernelGGL((packed_grad_bf16_kernel<DH, Pass::QUERIES>), dim3((unsigned)head_tile_blocks(a.s.n_heads, a.tiles)), dim3(256), (PackForm<DH, Pass::QUERIES>::LDS), st, a);
     BR_LAUNCH_CHECK();
-    return BR_OK;
-  };
-  const br_status ok = run(std::false_type{}, a.s.q_tokens, a.s.n_heads);
-  return ok != BR_OK ? ok : run(std::true_type{}, a.s.k_tokens, a.s.n_kv_heads);
+  }
+  if (a.s.k_tokens > 0) {
+    a.tiles = (int)doc_tiles_most(a.s.n_docs, a.s.k_tokens, PACK_OWN);
+    hipLaunchKernelGGL((packed_grad_bf16_kernel<DH, Pass::KEYS>), dim3((unsigned)head_tile_blocks(a.s.n_kv_heads, a.tiles)), dim3(256), (PackForm<DH, Pass::KEYS>::LDS), st, a);
+    BR_LAUNCH_CHECK();
+  }
+  return BR_OK;
 }
 
 br_status launch_attn_grad_bf16(AttnArgs a, hipStream_t st) { return a.s.head_dim == 64 ? grad_launch<64>(a, st) : grad_launch<128>(a, st); }
