@@ -33,9 +33,12 @@ static __device__ inline u32x4 buffer_rows(const void* p, unsigned bytes) {
                (unsigned)__builtin_amdgcn_readfirstlane(bytes), 0x00020000u};
 }
 
-// Slot permutation of a tile's rows: 16-byte chunk c of row r sits in slot c ^ tile_swz(r).
+// Slot permutation of a tile's rows: 16-byte chunk c of row r sits in slot c ^ tile_swz(r).  Transposed 8-byte reads are served 32 lanes at a time (eight rows
+// and two chunks: the rows, or with 128-byte rows the row pairs, take different pairs of slots).  16-byte reads are served in groups of lanes
+// {0-3, 12-15, 20-27} and {4-11, 16-19, 28-31} (and 32 further): with even permutations the quarters' neighbouring chunks fill the odd slots.  (Permutations that are
+// free of conflicts for 16 consecutive lanes instead: a third of the LDS's cycles were conflicts.)
 template <int DH>
-__device__ inline int tile_swz(int r) { return DH == 128 ? ((r & 7) << 1 | (r >> 3 & 1)) : ((r >> 1 & 3) << 1 | (r >> 3 & 1)); }
+__device__ inline int tile_swz(int r) { return DH == 128 ? (r & 7) << 1 : (r >> 1 & 3) << 1; }
 
 // Two matrices' rows on their way into LDS in tiles of PACK_TILE rows, those of the second behind those of the first: 1 KB an instruction, lane i fills bytes
 // 16 i .. 16 i + 15, so the permutation is applied on the global side; rows past the document's end lie past the buffer's and arrive as zeros.
