@@ -7,6 +7,7 @@ error, there is no fallback path.
 """
 import ctypes as C
 import os
+import struct
 
 import numpy as np
 
@@ -68,6 +69,7 @@ def load():
     for name in ("br_workspace_bytes", "br_reward_scratch_bytes", "br_sde_scratch_bytes", "br_sde_static_scratch_limit", "br_attention_workspace_bytes",
                  "br_layer_norm_workspace_bytes", "br_grpo_backward_workspace_bytes"):
         getattr(lib, name).restype = C.c_size_t
+    _train_types(lib)
     lib.br_tree_free.restype = None
     lib.br_model_free.restype = None
     _lib = lib
@@ -93,8 +95,10 @@ def _h(a, dtype):
 
 
 def _stream():
+    """The current stream of the current device, as its handle (the Stream object that torch.cuda.current_stream makes on the way costs 3 us, a launch 4)."""
     import torch
-    return C.c_void_p(torch.cuda.current_stream().cuda_stream)
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return C.c_void_p(raw(torch.cuda.current_device()) if raw else torch.cuda.current_stream().cuda_stream)
 
 
 class Tree:
@@ -344,96 +348,107 @@ class EdgeSet(C.Structure):
                 ("edge_ids", C.c_void_p), ("row_parent", C.c_void_p), ("row_first", C.c_void_p), ("row_coef", C.c_void_p)]
 
 
-class AdamwTensor(C.Structure):
-    _fields_ = [(n, C.c_void_p) for n in ("param", "grad", "m", "v", "m_scale", "v_scale", "copy")] + [("n", C.c_int64), ("weight_decay", C.c_double)]
+# The same as packed bytes, which the calls below pass (a structure filled field by field costs 2 us, a small call's kernels 4).
+_ATTN_SHAPE, _NORM_SHAPE, _EDGE_SET = struct.Struct("@7if7qPP"), struct.Struct("@8iPP"), struct.Struct("@q4if4x4P")
 
 
-class AdamwCfg(C.Structure):
-    _fields_ = [(n, C.c_double) for n in ("lr", "beta1", "beta2", "eps")] + [("step", C.c_int64), ("seed", C.c_uint64), ("grad_dtype", C.c_int32),
-                                                                            ("state_bits", C.c_int32), ("grad_scale", C.c_void_p)]
+def _train_types(lib):
+    """Argument types of the calls below: numbers pass as they are."""
+    p, z = C.c_void_p, C.c_size_t
+    for name, n in (("br_attention_forward", 7), ("br_attention_backward", 11), ("br_layer_norm_backward", 10), ("br_grpo_backward", 10)):
+        getattr(lib, name).argtypes = [p] * n + [z, p]
+    lib.br_layer_norm_forward.argtypes = [p] * 7
 
 
 def _dtype(x):
-    name = str(x.dtype)
-    assert name in ("torch.float32", "torch.bfloat16"), name
-    return F32 if name == "torch.float32" else BF16
+    import torch
+    if x.dtype is torch.bfloat16:
+        return BF16
+    assert x.dtype is torch.float32, x.dtype
+    return F32
 
 
 def _token_stride(x):
     """Elements between tokens of a [tokens, heads, head_dim] tensor whose heads are adjacent."""
     tokens, heads, d = x.shape
-    assert tokens == 0 or (x.stride(2) == 1 and (heads == 1 or x.stride(1) == d)), "heads of a token must be adjacent"
-    return x.stride(0) if tokens > 1 else heads * d
+    t, h, e = x.stride()
+    assert tokens == 0 or (e == 1 and (heads == 1 or h == d)), "heads of a token must be adjacent"
+    return t if tokens > 1 else heads * d
 
 
 def _flat(x, dtype=None):
-    """Device pointer of a contiguous tensor, as a number."""
+    """Device address of a contiguous tensor (None: 0)."""
     if x is None:
-        return None
-    assert x.is_contiguous() and (dtype is None or str(x.dtype) == dtype), (x.stride(), x.dtype)
+        return 0
+    assert x.is_contiguous() and (dtype is None or x.dtype is dtype), (x.stride(), x.dtype)
     return x.data_ptr()
 
 
 def _room(workspace):
-    return (C.c_void_p(0), C.c_size_t(0)) if workspace is None else (_p(workspace), C.c_size_t(workspace.numel() * workspace.element_size()))
+    return (0, 0) if workspace is None else (_flat(workspace), workspace.numel() * workspace.element_size())
 
 
 def _attn_shape(q, k, v, o, q_off, k_off, scale, dq=None, dk=None, dv=None):
-    assert q.dtype == k.dtype == v.dtype == o.dtype and k.shape == v.shape and q.shape == o.shape and q.shape[2] == k.shape[2], "shapes or types differ"
+    import torch
+    qs, ks = q.shape, k.shape
+    assert q.dtype is k.dtype is v.dtype is o.dtype and ks == v.shape and qs == o.shape and qs[2] == ks[2], "shapes or types differ"
     assert q_off.shape == k_off.shape and q_off.dim() == 1, "one offset more than documents"
-    s = AttnShape(_dtype(q), q.shape[1], k.shape[1], q.shape[2], q_off.shape[0] - 1, q.shape[0], k.shape[0], 0.0 if scale is None else scale,
-                  _token_stride(q), _token_stride(k), _token_stride(v), _token_stride(o), 0, 0, 0, _flat(q_off, "torch.int32"), _flat(k_off, "torch.int32"))
-    if dq is not None:
-        assert dq.shape == q.shape and dk.shape == k.shape and dv.shape == v.shape and dq.dtype == dk.dtype == dv.dtype == q.dtype, "shapes or types differ"
-        s.dq_stride, s.dk_stride, s.dv_stride = _token_stride(dq), _token_stride(dk), _token_stride(dv)
-    return s
+    if dq is None:
+        grads = (0, 0, 0)
+    else:
+        assert dq.shape == qs and dk.shape == ks and dv.shape == ks and dq.dtype is dk.dtype is dv.dtype is q.dtype, "shapes or types differ"
+        grads = (_token_stride(dq), _token_stride(dk), _token_stride(dv))
+    return _ATTN_SHAPE.pack(_dtype(q), qs[1], ks[1], qs[2], q_off.shape[0] - 1, qs[0], ks[0], 0.0 if scale is None else scale, _token_stride(q), _token_stride(k), _token_stride(v),
+                            _token_stride(o), *grads, _flat(q_off, torch.int32), _flat(k_off, torch.int32))
 
 
 def attention_workspace_bytes(q, k, v, q_off, k_off, backward):
-    s = _attn_shape(q, k, v, q, q_off, k_off, None, *((q, k, v) if backward else ()))
-    return load().br_attention_workspace_bytes(C.byref(s), C.c_int32(1 if backward else 0))
+    return load().br_attention_workspace_bytes(_attn_shape(q, k, v, q, q_off, k_off, None, *((q, k, v) if backward else ())), 1 if backward else 0)
 
 
 def attention_forward(q, k, v, q_off, k_off, out, lse, workspace=None, scale=None):
     """q, out [tokens, heads, head_dim], k, v [tokens, kv heads, head_dim] (tokens may be strided), offsets int32 [documents + 1], lse [heads, tokens] fp32."""
+    import torch
     s = _attn_shape(q, k, v, out, q_off, k_off, scale)
-    assert tuple(lse.shape) == (q.shape[1], q.shape[0])
-    _check(load().br_attention_forward(C.byref(s), C.c_void_p(q.data_ptr()), C.c_void_p(k.data_ptr()), C.c_void_p(v.data_ptr()), C.c_void_p(out.data_ptr()),
-                                       C.c_void_p(_flat(lse, "torch.float32")), *_room(workspace), _stream()))
+    assert lse.shape == (q.shape[1], q.shape[0])
+    _check(load().br_attention_forward(s, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _flat(lse, torch.float32), *_room(workspace), _stream()))
 
 
 def attention_backward(dout, q, k, v, out, lse, q_off, k_off, dq, dk, dv, workspace, scale=None):
+    """dout laid out as out; dq, dk, dv may be strided (parts of one gradient)."""
+    import torch
     s = _attn_shape(q, k, v, out, q_off, k_off, scale, dq, dk, dv)
-    assert dout.shape == out.shape and dout.dtype == out.dtype and _token_stride(dout) == s.o_stride, "dout must be laid out as out"
-    assert tuple(lse.shape) == (q.shape[1], q.shape[0])
-    _check(load().br_attention_backward(C.byref(s), *[C.c_void_p(x.data_ptr()) for x in (dout, q, k, v, out)], C.c_void_p(_flat(lse, "torch.float32")),
-                                        *[C.c_void_p(x.data_ptr()) for x in (dq, dk, dv)], *_room(workspace), _stream()))
+    assert dout.shape == out.shape and dout.dtype is out.dtype and _token_stride(dout) == _token_stride(out), "dout must be laid out as out"
+    assert lse.shape == (q.shape[1], q.shape[0])
+    _check(load().br_attention_backward(s, dout.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _flat(lse, torch.float32), dq.data_ptr(), dk.data_ptr(),
+                                        dv.data_ptr(), *_room(workspace), _stream()))
 
 
 def _norm_shape(x, y, mods, shift_off, scale_off, row_off, group):
-    assert x.shape == y.shape and group.shape[0] == row_off.shape[0] - 1, "shapes differ"
-    return NormShape(_dtype(y), x.shape[0], x.shape[1], group.shape[0], mods.shape[0], mods.shape[1], shift_off, scale_off, _flat(row_off, "torch.int32"),
-                     _flat(group, "torch.int32"))
+    import torch
+    docs = group.shape[0]
+    assert x.shape == y.shape and docs == row_off.shape[0] - 1, "shapes differ"
+    return _NORM_SHAPE.pack(_dtype(y), *x.shape, docs, *mods.shape, shift_off, scale_off, _flat(row_off, torch.int32), _flat(group, torch.int32))
 
 
 def layer_norm_workspace_bytes(x, dout, mods, shift_off, scale_off, row_off, group):
-    s = _norm_shape(x, dout, mods, shift_off, scale_off, row_off, group)
-    return load().br_layer_norm_workspace_bytes(C.byref(s))
+    return load().br_layer_norm_workspace_bytes(_norm_shape(x, dout, mods, shift_off, scale_off, row_off, group))
 
 
 def layer_norm_forward(x, mods, shift_off, scale_off, row_off, group, out, mean=None, rstd=None):
-    s = _norm_shape(x, out, mods, shift_off, scale_off, row_off, group)
+    """x [rows, hidden] fp32, mods [groups, stride] fp32, out [rows, hidden]; mean, rstd [rows] fp32 or both None."""
+    import torch
+    s, f = _norm_shape(x, out, mods, shift_off, scale_off, row_off, group), torch.float32
     assert mean is None or mean.numel() == rstd.numel() == x.shape[0]
-    f = "torch.float32"
-    _check(load().br_layer_norm_forward(C.byref(s), C.c_void_p(_flat(x, f)), C.c_void_p(_flat(mods, f)), C.c_void_p(_flat(out)), C.c_void_p(_flat(mean, f)), C.c_void_p(_flat(rstd, f)),
-                                        _stream()))
+    _check(load().br_layer_norm_forward(s, _flat(x, f), _flat(mods, f), _flat(out), _flat(mean, f), _flat(rstd, f), _stream()))
 
 
 def layer_norm_backward(dout, x, mean, rstd, mods, shift_off, scale_off, row_off, group, residual, dx, dmods, workspace):
-    s = _norm_shape(x, dout, mods, shift_off, scale_off, row_off, group)
+    """residual: the gradient that reaches x past the norm, or None; dx may be the same tensor."""
+    import torch
+    s, f = _norm_shape(x, dout, mods, shift_off, scale_off, row_off, group), torch.float32
     assert dx.shape == x.shape and dmods.shape == mods.shape and mean.numel() == rstd.numel() == x.shape[0] and (residual is None or residual.shape == x.shape)
-    f = "torch.float32"
-    _check(load().br_layer_norm_backward(C.byref(s), C.c_void_p(_flat(dout)), *[C.c_void_p(_flat(t, f)) for t in (x, mean, rstd, mods, residual, dx, dmods)], *_room(workspace),
+    _check(load().br_layer_norm_backward(s, _flat(dout), _flat(x, f), _flat(mean, f), _flat(rstd, f), _flat(mods, f), _flat(residual, f), _flat(dx, f), _flat(dmods, f), *_room(workspace),
                                          _stream()))
 
 
@@ -449,23 +464,32 @@ def edge_rows(tree, sched, D, edge_ids):
 
 
 def _edge_set(z_nodes, v_rows, edge_ids, row_parent, row_first, row_coef, clip_eps, n_total):
-    i32 = "torch.int32"
-    assert z_nodes.shape[1] == v_rows.shape[1] and row_parent.shape[0] == v_rows.shape[0] == row_first.shape[0] - 1 and row_coef.numel() == 4 * row_parent.shape[0], "shapes differ"
-    return EdgeSet(z_nodes.shape[1], z_nodes.shape[0], row_parent.shape[0], edge_ids.shape[0], n_total, clip_eps, _flat(edge_ids, i32), _flat(row_parent, i32), _flat(row_first, i32),
-                   _flat(row_coef, "torch.float64"))
+    import torch
+    i32, (nodes, D), rows = torch.int32, z_nodes.shape, row_parent.shape[0]
+    assert v_rows.shape == (rows, D) and row_first.shape[0] == rows + 1 and row_coef.numel() == 4 * rows, "shapes differ"
+    return _EDGE_SET.pack(D, nodes, rows, edge_ids.shape[0], n_total, clip_eps, _flat(edge_ids, i32), _flat(row_parent, i32), _flat(row_first, i32), _flat(row_coef, torch.float64))
 
 
 def grpo_backward_workspace_bytes(z_nodes, v_rows, edge_ids, row_parent, row_first, row_coef):
-    s = _edge_set(z_nodes, v_rows, edge_ids, row_parent, row_first, row_coef, 0.0, 0)
-    return load().br_grpo_backward_workspace_bytes(C.byref(s))
+    return load().br_grpo_backward_workspace_bytes(_edge_set(z_nodes, v_rows, edge_ids, row_parent, row_first, row_coef, 0.0, 0))
 
 
 def grpo_backward(z_nodes, v_rows, edge_ids, row_parent, row_first, row_coef, logp_old_nodes, adv_nodes, clip_eps, J, logp_new, grad_v, workspace, clipped=None, n_total=0):
-    s = _edge_set(z_nodes, v_rows, edge_ids, row_parent, row_first, row_coef, clip_eps, n_total)
+    """Tables as edge_rows gives them, on the device; logp_new [edges], grad_v like v_rows, clipped uint8 [edges] or None."""
+    import torch
+    s, f = _edge_set(z_nodes, v_rows, edge_ids, row_parent, row_first, row_coef, clip_eps, n_total), torch.float32
     assert grad_v.shape == v_rows.shape and logp_new.shape == edge_ids.shape and logp_old_nodes.numel() == adv_nodes.numel() == z_nodes.shape[0], "shapes differ"
-    f = "torch.float32"
-    _check(load().br_grpo_backward(C.byref(s), *[C.c_void_p(_flat(t, f)) for t in (z_nodes, v_rows, logp_old_nodes, adv_nodes, J, logp_new, grad_v)], C.c_void_p(_flat(clipped)),
-                                   *_room(workspace), _stream()))
+    _check(load().br_grpo_backward(s, _flat(z_nodes, f), _flat(v_rows, f), _flat(logp_old_nodes, f), _flat(adv_nodes, f), _flat(J, f), _flat(logp_new, f), _flat(grad_v, f),
+                                   _flat(clipped), *_room(workspace), _stream()))
+
+
+class AdamwTensor(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("param", "grad", "m", "v", "m_scale", "v_scale", "copy")] + [("n", C.c_int64), ("weight_decay", C.c_double)]
+
+
+class AdamwCfg(C.Structure):
+    _fields_ = [(n, C.c_double) for n in ("lr", "beta1", "beta2", "eps")] + [("step", C.c_int64), ("seed", C.c_uint64), ("grad_dtype", C.c_int32),
+                                                                            ("state_bits", C.c_int32), ("grad_scale", C.c_void_p)]
 
 
 class AdamW:
@@ -473,19 +497,20 @@ class AdamW:
     fp32, or uint8 codes with m_scales, v_scales (fp32, one of 256 elements); copies: bf16 tensors that receive the rounded parameters, or None."""
 
     def __init__(self, params, grads, m, v, m_scales=None, v_scales=None, copies=None, weight_decay=0.01, lr=1e-4, betas=(0.9, 0.999), eps=1e-8, seed=0, step=0):
+        import torch
         n = len(params)
         none = [None] * n
         bits = 32 if m_scales is None else 8
-        state = "torch.float32" if bits == 32 else "torch.uint8"
+        state = torch.float32 if bits == 32 else torch.uint8
         decay = [weight_decay] * n if isinstance(weight_decay, (int, float)) else list(weight_decay)
         self.tensors = (AdamwTensor * max(n, 1))()
         self.n, self._keep = n, (params, grads, m, v, m_scales, v_scales, copies)
-        f = "torch.float32"
+        f = torch.float32
         for i, (p, g, mm, vv, ms, vs, c, w) in enumerate(zip(params, grads, m, v, m_scales or none, v_scales or none, copies or none, decay, strict=True)):
             k = p.numel()
             assert g.numel() == mm.numel() == vv.numel() == k and (c is None or c.numel() == k) and (ms is None or ms.numel() == vs.numel() == (k + 255) // 256), "sizes differ"
             assert g.dtype == grads[0].dtype
-            self.tensors[i] = AdamwTensor(_flat(p, f), _flat(g), _flat(mm, state), _flat(vv, state), _flat(ms, f), _flat(vs, f), _flat(c, "torch.bfloat16"), k, w)
+            self.tensors[i] = AdamwTensor(_flat(p, f), _flat(g), _flat(mm, state), _flat(vv, state), _flat(ms, f), _flat(vs, f), _flat(c, torch.bfloat16), k, w)
         self.cfg = AdamwCfg(lr, betas[0], betas[1], eps, step, seed, _dtype(grads[0]) if n else F32, bits, None)
 
     def step(self, lr=None, grad_scale=None):
@@ -493,7 +518,7 @@ class AdamW:
         if lr is not None:
             self.cfg.lr = lr
         self.cfg.step += 1
-        self.cfg.grad_scale = _flat(grad_scale, "torch.float32")
+        self.cfg.grad_scale = None if grad_scale is None else _p(grad_scale).value
         code = load().br_adamw_step(C.byref(self.cfg), self.tensors, C.c_int32(self.n), _stream())
         if code != 0:
             self.cfg.step -= 1
@@ -501,6 +526,7 @@ class AdamW:
 
     def state_values(self, m_out, v_out):
         """The values that states in 8 bits stand for, into fp32 tensors."""
-        pointers = [(C.c_void_p * max(self.n, 1))(*[_flat(x, "torch.float32") for x in out]) for out in (m_out, v_out)]
+        import torch
+        pointers = [(C.c_void_p * max(self.n, 1))(*[_flat(x, torch.float32) for x in out]) for out in (m_out, v_out)]
         assert all(x.numel() == t.n for out in (m_out, v_out) for x, t in zip(out, self.tensors))
         _check(load().br_adamw_state_values(self.tensors, C.c_int32(self.n), *pointers, _stream()))

@@ -162,3 +162,9 @@ def test_edge_rows_refuse():
     with pytest.raises(br.BranchRolloutError):
         br.edge_rows(t, synth.schedule(5, 3.0), 8, [1])
     assert [len(x) for x in br.edge_rows(t, sched, 8, [])] == [0, 1, 0]
+
+
+def test_packed_shapes_are_laid_out_as_the_structures():
+    for packed, fields in ((br._ATTN_SHAPE, br.AttnShape), (br._NORM_SHAPE, br.NormShape), (br._EDGE_SET, br.EdgeSet)):
+        values = [k + 1 for k in range(len(fields._fields_))]
+        assert packed.size == C.sizeof(fields) and [getattr(fields.from_buffer_copy(packed.pack(*values)), n) for n, _ in fields._fields_] == values
