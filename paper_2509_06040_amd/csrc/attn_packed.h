@@ -53,6 +53,16 @@ __device__ inline bool head_tile(int heads, int tiles, int* head, int* tile) {
   return *tile < tiles;
 }
 
+// Tiles of `rows` own rows over all heads: sets a.tiles; workgroups of the launch.
+inline br_status attn_grid(AttnArgs& a, int tokens, int heads, int rows, unsigned* blocks) {
+  const long long tiles = doc_tiles_most(a.s.n_docs, tokens, rows);
+  a.tiles = (int)tiles;
+  const long long n = tiles < 0x7FFFFFFFLL ? head_tile_blocks(heads, a.tiles) : 0x7FFFFFFFLL;
+  BR_REQUIRE(n < 0x7FFFFFFFLL, BR_ESHAPE, "attention: too many workgroups for one launch");
+  *blocks = (unsigned)n;
+  return BR_OK;
+}
+
 // ---- attn_packed_bf16.hip
 bool attn_packed_bf16_fits(const br_attn_shape& s);
 br_status launch_attn_forward_bf16(AttnArgs a, hipStream_t st);

@@ -548,8 +548,10 @@ bool attn_packed_bf16_fits(const br_attn_shape& s) {
 }
 
 br_status launch_attn_forward_bf16(AttnArgs a, hipStream_t st) {
-  a.tiles = (int)doc_tiles_most(a.s.n_docs, a.s.q_tokens, PACK_OWN);
-  const dim3 grid((unsigned)head_tile_blocks(a.s.n_heads, a.tiles));
+  unsigned n;
+  const br_status ok = attn_grid(a, a.s.q_tokens, a.s.n_heads, PACK_OWN, &n);
+  if (ok != BR_OK) return ok;
+  const dim3 grid(n);
   if (a.s.head_dim == 64) hipLaunchKernelGGL((packed_forward_bf16_kernel<64>), grid, dim3(256), (PackForm<64, Pass::FORWARD>::LDS), st, a);
   else hipLaunchKernelGGL((packed_forward_bf16_kernel<128>), grid, dim3(256), (PackForm<128, Pass::FORWARD>::LDS), st, a);
   BR_LAUNCH_CHECK();
@@ -558,14 +560,17 @@ br_status launch_attn_forward_bf16(AttnArgs a, hipStream_t st) {
 
 template <int DH>
 static br_status grad_launch(AttnArgs a, hipStream_t st) {
+  unsigned n;
   if (a.s.q_tokens > 0) {
-    a.tiles = (int)doc_tiles_most(a.s.n_docs, a.s.q_tokens, PACK_OWN);
-    hipLaunchKernelGGL((packed_grad_bf16_kernel<DH, Pass::QUERIES>), dim3((unsigned)head_tile_blocks(a.s.n_heads, a.tiles)), dim3(256), (PackForm<DH, Pass::QUERIES>::LDS), st, a);
+    const br_status ok = attn_grid(a, a.s.q_tokens, a.s.n_heads, PACK_OWN, &n);
+    if (ok != BR_OK) return ok;
+    hipLaunchKernelGGL((packed_grad_bf16_kernel<DH, Pass::QUERIES>), dim3(n), dim3(256), (PackForm<DH, Pass::QUERIES>::LDS), st, a);
     BR_LAUNCH_CHECK();
   }
   if (a.s.k_tokens > 0) {
-    a.tiles = (int)doc_tiles_most(a.s.n_docs, a.s.k_tokens, PACK_OWN);
-    hipLaunchKernelGGL((packed_grad_bf16_kernel<DH, Pass::KEYS>), dim3((unsigned)head_tile_blocks(a.s.n_kv_heads, a.tiles)), dim3(256), (PackForm<DH, Pass::KEYS>::LDS), st, a);
+    const br_status ok = attn_grid(a, a.s.k_tokens, a.s.n_kv_heads, PACK_OWN, &n);
+    if (ok != BR_OK) return ok;
+    hipLaunchKernelGGL((packed_grad_bf16_kernel<DH, Pass::KEYS>), dim3(n), dim3(256), (PackForm<DH, Pass::KEYS>::LDS), st, a);
     BR_LAUNCH_CHECK();
   }
   return BR_OK;

@@ -1,9 +1,12 @@
-// Attention over packed documents with its backward pass: the forms that hold for every type and head dim.
+// Attention over packed documents with its backward pass: the forms that hold for every type and head dim (fp32; bf16 where offsets pass 32 bits).
 //
-// A wavefront keeps 16 rows of one side in registers (queries forward and for dq, keys for dk and dv) and walks the rows of the other side in tiles
-// that the workgroup stages in LDS.  Scores are taken so that a lane holds four rows of the tile for ONE row of its own per block of 16 (C layout of the 16x16
-// matrix instructions); exponentiated, these registers are, without moving, the column operand of the products that contract over the tile's rows, whose row
-// operand is read from LDS transposed.
+// A wavefront keeps 16 rows of one side in registers (queries forward and for dq, keys for dk and dv) and walks the rows of the other side in tiles of 64
+// that the workgroup stages in LDS, the next tile on its way in registers meanwhile.  Scores are taken so that a lane holds four rows of the tile for ONE row of
+// its own per block of 16 (C layout of the 16x16 matrix instructions); exponentiated, these registers are, without moving, the column operand of the
+// products that contract over the tile's rows, whose row operand is read from LDS transposed.
+//
+// WIDE: the four wavefronts have 16 own rows each and all of the tile.  Otherwise (fp32 launches that would leave compute units empty) they share 16 own rows and
+// take 16 rows of the tile each; their sums are joined through LDS at the end.
 #include "attn_packed.h"
 
 namespace br {
@@ -36,16 +39,28 @@ struct Tile {
   static constexpr int ROW = DH * (int)sizeof(T) + (sizeof(T) == 4 ? 16 : 0), BYTES = TILE_ROWS * ROW, CH = DH * (int)sizeof(T) / 16;
   static __device__ inline int chunk(int r, int c) {
     if constexpr (sizeof(T) == 4) return r * ROW + c * 16;
-    const int f = DH == 128 ? ((r & 7) << 1 | (r >> 3 & 1)) : ((r >> 1 & 3) << 1 | (r >> 3 & 1));
+    const int f = DH == 128 ? (r & 7) << 1 : (r >> 1 & 3) << 1;
     return r * ROW + ((c ^ f) << 4);
   }
+  static constexpr int EACH = TILE_ROWS * CH / 256;  // 16-byte chunks a thread
+  static_assert(TILE_ROWS * CH % 256 == 0, "");
+  struct Regs {
+    f32x4 v[EACH];
+  };
   // rows first .. first + 63 (those from `end` on: zeros) of a matrix with `stride` elements a row
-  static __device__ inline void stage(char* lds, const T* p, size_t stride, int first, int end) {
-    for (int i = threadIdx.x; i < TILE_ROWS * CH; i += 256) {
-      const int r = i / CH, c = i - r * CH;
-      f32x4 v = {0.f, 0.f, 0.f, 0.f};
-      if (first + r < end) v = *reinterpret_cast<const f32x4*>(reinterpret_cast<const char*>(p + (size_t)(first + r) * stride) + c * 16);
-      *reinterpret_cast<f32x4*>(lds + chunk(r, c)) = v;
+  static __device__ inline void fetch(Regs& r, const T* p, size_t stride, int first, int end) {
+#pragma unroll
+    for (int k = 0; k < EACH; ++k) {
+      const int i = k * 256 + threadIdx.x, row = i / CH, c = i - row * CH;
+      r.v[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (first + row < end) r.v[k] = *reinterpret_cast<const f32x4*>(reinterpret_cast<const char*>(p + (size_t)(first + row) * stride) + c * 16);
+    }
+  }
+  static __device__ inline void put(char* lds, const Regs& r) {
+#pragma unroll
+    for (int k = 0; k < EACH; ++k) {
+      const int i = k * 256 + threadIdx.x, row = i / CH, c = i - row * CH;
+      *reinterpret_cast<f32x4*>(lds + chunk(row, c)) = r.v[k];
     }
   }
   // row operand: rows 16 blk + lane % 16, contraction over the channels of step ks
@@ -83,7 +98,7 @@ static __device__ inline void own_rows(typename Op<T>::Frag (&f)[DH / (4 * Op<T>
 }
 // Step ks of a contraction over the tile's rows: blocks of 16 rows in the C layout, in the type of the operands.
 template <typename T>
-static __device__ inline typename Op<T>::Frag step_of(const f32x4 (&p)[4], int ks) {
+static __device__ inline typename Op<T>::Frag step_of(const f32x4* p, int ks) {
   if constexpr (sizeof(T) == 2) {
     bf16x8 f;
 #pragma unroll
@@ -94,18 +109,48 @@ static __device__ inline typename Op<T>::Frag step_of(const f32x4 (&p)[4], int k
   }
 }
 
-template <typename T, int DH>
-__global__ __launch_bounds__(256) void packed_attention_kernel(AttnArgs a) {
+// WIDE: each wavefront's blocks d of 16 channels, else their sums over the four wavefronts (in their order; block d by wavefront d % 4).  f(d, values).
+template <int DB, bool WIDE, typename F>
+static __device__ inline void joined(char* lds, const f32x4 (&acc)[DB], F f) {
+  if constexpr (WIDE) {
+#pragma unroll
+    for (int d = 0; d < DB; ++d) f(d, acc[d]);
+  } else {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    f32x4* to = reinterpret_cast<f32x4*>(lds);
+    __syncthreads();
+#pragma unroll
+    for (int d = 0; d < DB; ++d) to[(wave * DB + d) * 64 + lane] = acc[d];
+    __syncthreads();
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+      if (d % 4 == wave) f(d, (to[d * 64 + lane] + to[(DB + d) * 64 + lane]) + (to[(2 * DB + d) * 64 + lane] + to[(3 * DB + d) * 64 + lane]));
+  }
+}
+
+template <typename T, int DH, bool WIDE>
+struct Kernel {  // sizes of the kernels below
   using O = Op<T>;
   using L = Tile<T, DH>;
-  constexpr int KS = DH / (4 * O::EPL), PS = TILE_ROWS / (4 * O::EPL), DB = DH / 16;
+  static constexpr int KS = DH / (4 * O::EPL), DB = DH / 16, OWN = WIDE ? 64 : 16;
+  static constexpr int NB = WIDE ? 4 : 1, PS = 16 * NB / (4 * O::EPL);  // blocks of 16 rows of the tile a wavefront takes, steps over them
+  static_assert(WIDE || O::EPL == 4, "");
+};
+
+template <typename T, int DH, bool WIDE>
+__global__ __launch_bounds__(256) void packed_attention_kernel(AttnArgs a) {
+  using K = Kernel<T, DH, WIDE>;
+  using O = Op<T>;
+  using L = Tile<T, DH>;
+  constexpr int KS = K::KS, PS = K::PS, DB = K::DB, NB = K::NB;
   __shared__ __attribute__((aligned(16))) char lds[2 * L::BYTES];
+  __shared__ float tops[4][16], sums[4][16];
   DocSpan span;
   int first, head, tile;
-  if (!head_tile(a.s.n_heads, a.tiles, &head, &tile) || !doc_tile(a.s.q_off, a.s.n_docs, a.s.q_tokens, 64, tile, &span, &first)) return;
+  if (!head_tile(a.s.n_heads, a.tiles, &head, &tile) || !doc_tile(a.s.q_off, a.s.n_docs, a.s.q_tokens, K::OWN, tile, &span, &first)) return;
   const DocSpan keys = other_rows(a.s.k_off, a.s.n_docs, a.s.k_tokens, span);
-  const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4, kv = head / (a.s.n_heads / a.s.n_kv_heads);
-  const int row = first + (threadIdx.x >> 6) * 16 + l16;
+  const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), kv = head / (a.s.n_heads / a.s.n_kv_heads);
+  const int row = first + (WIDE ? wave * 16 : 0) + l16, b0 = WIDE ? 0 : wave;
   const T *k = (const T*)a.k + (size_t)kv * DH, *v = (const T*)a.v + (size_t)kv * DH;
   typename O::Frag q[KS];
   own_rows<T, DH>(q, (const T*)a.q + (size_t)head * DH, a.s.q_stride, row, span.end);
@@ -114,29 +159,36 @@ __global__ __launch_bounds__(256) void packed_attention_kernel(AttnArgs a) {
   for (int d = 0; d < DB; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
   float top = -INFINITY, sum = 0.f;
   const float unit = a.scale * LOG2E;  // scores in powers of two
+  typename L::Regs nk, nv;
+  L::fetch(nk, k, a.s.k_stride, keys.first, keys.end);
+  L::fetch(nv, v, a.s.v_stride, keys.first, keys.end);
   for (int k0 = keys.first; k0 < keys.end; k0 += TILE_ROWS) {
     __syncthreads();
-    L::stage(lds, k, a.s.k_stride, k0, keys.end);
-    L::stage(lds + L::BYTES, v, a.s.v_stride, k0, keys.end);
+    L::put(lds, nk);
+    L::put(lds + L::BYTES, nv);
     __syncthreads();
-    f32x4 p[4];
+    L::fetch(nk, k, a.s.k_stride, k0 + TILE_ROWS, keys.end);
+    L::fetch(nv, v, a.s.v_stride, k0 + TILE_ROWS, keys.end);
+    f32x4 p[NB];
     float most = -INFINITY;
 #pragma unroll
-    for (int b = 0; b < 4; ++b) {
-      p[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int b = 0; b < NB; ++b) p[b] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) p[b] = O::mma(L::rows(lds, b, ks), q[ks], p[b]);
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+      for (int b = 0; b < NB; ++b) p[b] = O::mma(L::rows(lds, b0 + b, ks), q[ks], p[b]);
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        p[b][r] = k0 + b * 16 + 4 * g + r < keys.end ? p[b][r] * unit : -INFINITY;
+        p[b][r] = k0 + (b0 + b) * 16 + 4 * g + r < keys.end ? p[b][r] * unit : -INFINITY;
         most = __builtin_elementwise_maximum(most, p[b][r]);
       }
-    }
     const float next = __builtin_elementwise_maximum(top, quarters_max(most)), ref = next == -INFINITY ? 0.f : next;
     const float shrink = __builtin_amdgcn_exp2f(top - ref);
     float part = 0.f;
 #pragma unroll
-    for (int b = 0; b < 4; ++b)
+    for (int b = 0; b < NB; ++b)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         p[b][r] = __builtin_amdgcn_exp2f(p[b][r] - ref);
@@ -150,32 +202,51 @@ __global__ __launch_bounds__(256) void packed_attention_kernel(AttnArgs a) {
     for (int ks = 0; ks < PS; ++ks) {
       const typename O::Frag pf = step_of<T>(p, ks);
 #pragma unroll
-      for (int d = 0; d < DB; ++d) o[d] = O::mma(L::cols(lds + L::BYTES, ks, d), pf, o[d]);
+      for (int d = 0; d < DB; ++d) o[d] = O::mma(L::cols(lds + L::BYTES, b0 + ks, d), pf, o[d]);
     }
   }
   sum = quarters_sum(sum);
-  if (row >= span.end) return;
+  if constexpr (!WIDE) {  // one reference for the four wavefronts
+    if (g == 0) {
+      tops[wave][l16] = top;
+      sums[wave][l16] = sum;
+    }
+    __syncthreads();
+    const float most = __builtin_elementwise_maximum(__builtin_elementwise_maximum(tops[0][l16], tops[1][l16]), __builtin_elementwise_maximum(tops[2][l16], tops[3][l16]));
+    const float ref = most == -INFINITY ? 0.f : most, shrink = __builtin_amdgcn_exp2f(top - ref);
+#pragma unroll
+    for (int d = 0; d < DB; ++d) o[d] *= shrink;
+    sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) sum += sums[w][l16] * __builtin_amdgcn_exp2f(tops[w][l16] - ref);
+    top = most;
+  }
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
   T* out = (T*)a.o + (size_t)row * a.s.o_stride + (size_t)head * DH + 4 * g;
-#pragma unroll
-  for (int d = 0; d < DB; ++d) store4(out + 16 * d, o[d][0] * inv, o[d][1] * inv, o[d][2] * inv, o[d][3] * inv);
-  if (g == 0) a.lse[(size_t)head * a.s.q_tokens + row] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * LN2;
+  joined<DB, WIDE>(lds, o, [&](int d, f32x4 x) {
+    if (row < span.end) store4(out + 16 * d, x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
+  });
+  if (row < span.end && g == 0 && (WIDE || wave == 0)) a.lse[(size_t)head * a.s.q_tokens + row] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * LN2;
 }
 
 // dq, and ref and delta for the kernel of dk and dv.
-template <typename T, int DH>
+template <typename T, int DH, bool WIDE>
 __global__ __launch_bounds__(256) void packed_attention_dq_kernel(AttnArgs a) {
+  using K = Kernel<T, DH, WIDE>;
   using O = Op<T>;
   using L = Tile<T, DH>;
-  constexpr int KS = DH / (4 * O::EPL), PS = TILE_ROWS / (4 * O::EPL), DB = DH / 16;
+  constexpr int KS = K::KS, PS = K::PS, DB = K::DB, NB = K::NB;
   __shared__ __attribute__((aligned(16))) char lds[2 * L::BYTES];
   DocSpan span;
   int first, head, tile;
-  if (!head_tile(a.s.n_heads, a.tiles, &head, &tile) || !doc_tile(a.s.q_off, a.s.n_docs, a.s.q_tokens, 64, tile, &span, &first)) return;
+  if (!head_tile(a.s.n_heads, a.tiles, &head, &tile) || !doc_tile(a.s.q_off, a.s.n_docs, a.s.q_tokens, K::OWN, tile, &span, &first)) return;
   const DocSpan keys = other_rows(a.s.k_off, a.s.n_docs, a.s.k_tokens, span);
-  const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4, kv = head / (a.s.n_heads / a.s.n_kv_heads);
-  const int row = first + (threadIdx.x >> 6) * 16 + l16;
+  const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), kv = head / (a.s.n_heads / a.s.n_kv_heads);
+  const int row = first + (WIDE ? wave * 16 : 0) + l16, b0 = WIDE ? 0 : wave;
   const T *k = (const T*)a.k + (size_t)kv * DH, *v = (const T*)a.v + (size_t)kv * DH;
+  typename L::Regs nk, nv;
+  L::fetch(nk, k, a.s.k_stride, keys.first, keys.end);
+  L::fetch(nv, v, a.s.v_stride, keys.first, keys.end);
   typename O::Frag q[KS], dout[KS];
   own_rows<T, DH>(q, (const T*)a.q + (size_t)head * DH, a.s.q_stride, row, span.end);
   own_rows<T, DH>(dout, (const T*)a.dout + (size_t)head * DH, a.s.o_stride, row, span.end);
@@ -192,7 +263,7 @@ __global__ __launch_bounds__(256) void packed_attention_dq_kernel(AttnArgs a) {
       const size_t at = (size_t)head * a.s.q_tokens + row;
       const float lse = a.lse[at];
       if (lse != -INFINITY) ref = lse * LOG2E;
-      if (g == 0) {
+      if (g == 0 && (WIDE || wave == 0)) {
         a.ref[at] = ref;
         a.delta[at] = delta;
       }
@@ -204,51 +275,69 @@ __global__ __launch_bounds__(256) void packed_attention_dq_kernel(AttnArgs a) {
   const float unit = a.scale * LOG2E;
   for (int k0 = keys.first; k0 < keys.end; k0 += TILE_ROWS) {
     __syncthreads();
-    L::stage(lds, k, a.s.k_stride, k0, keys.end);
-    L::stage(lds + L::BYTES, v, a.s.v_stride, k0, keys.end);
+    L::put(lds, nk);
+    L::put(lds + L::BYTES, nv);
     __syncthreads();
-    f32x4 ds[4];
+    L::fetch(nk, k, a.s.k_stride, k0 + TILE_ROWS, keys.end);
+    L::fetch(nv, v, a.s.v_stride, k0 + TILE_ROWS, keys.end);
+    f32x4 s[NB], ds[NB];
 #pragma unroll
-    for (int b = 0; b < 4; ++b) {
-      f32x4 s = {0.f, 0.f, 0.f, 0.f}, dp = {0.f, 0.f, 0.f, 0.f};
+    for (int b = 0; b < NB; ++b) s[b] = ds[b] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        s = O::mma(L::rows(lds, b, ks), q[ks], s);
-        dp = O::mma(L::rows(lds + L::BYTES, b, ks), dout[ks], dp);
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        s[b] = O::mma(L::rows(lds, b0 + b, ks), q[ks], s[b]);
+        ds[b] = O::mma(L::rows(lds + L::BYTES, b0 + b, ks), dout[ks], ds[b]);
       }
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const float p = __builtin_amdgcn_exp2f(fmaf(s[r], unit, -ref));
-        ds[b][r] = k0 + b * 16 + 4 * g + r < keys.end ? p * (dp[r] - delta) : 0.f;
+        const float p = __builtin_amdgcn_exp2f(fmaf(s[b][r], unit, -ref));
+        ds[b][r] = k0 + (b0 + b) * 16 + 4 * g + r < keys.end ? p * (ds[b][r] - delta) : 0.f;
       }
-    }
 #pragma unroll
     for (int ks = 0; ks < PS; ++ks) {
       const typename O::Frag f = step_of<T>(ds, ks);
 #pragma unroll
-      for (int d = 0; d < DB; ++d) dq[d] = O::mma(L::cols(lds, ks, d), f, dq[d]);
+      for (int d = 0; d < DB; ++d) dq[d] = O::mma(L::cols(lds, b0 + ks, d), f, dq[d]);
     }
   }
-  if (row >= span.end) return;
   T* to = (T*)a.dq + (size_t)row * a.s.dq_stride + (size_t)head * DH + 4 * g;
-#pragma unroll
-  for (int d = 0; d < DB; ++d) store4(to + 16 * d, dq[d][0] * a.scale, dq[d][1] * a.scale, dq[d][2] * a.scale, dq[d][3] * a.scale);
+  joined<DB, WIDE>(lds, dq, [&](int d, f32x4 x) {
+    if (row < span.end) store4(to + 16 * d, x[0] * a.scale, x[1] * a.scale, x[2] * a.scale, x[3] * a.scale);
+  });
 }
 
-// dk and dv of 64 keys, over the queries of all heads that share them.
-template <typename T, int DH>
+// dk and dv, over the queries of all heads that share the keys.
+template <typename T, int DH, bool WIDE>
 __global__ __launch_bounds__(256) void packed_attention_dkv_kernel(AttnArgs a) {
+  using K = Kernel<T, DH, WIDE>;
   using O = Op<T>;
   using L = Tile<T, DH>;
-  constexpr int KS = DH / (4 * O::EPL), PS = TILE_ROWS / (4 * O::EPL), DB = DH / 16;
+  constexpr int KS = K::KS, PS = K::PS, DB = K::DB, NB = K::NB;
   __shared__ __attribute__((aligned(16))) char lds[2 * L::BYTES];
-  __shared__ __attribute__((aligned(16))) float refs[2 * TILE_ROWS];  // lse in powers of two (infinite where there is no query), delta
+  __shared__ __attribute__((aligned(16))) float refs[2 * TILE_ROWS];  // ref (infinite where there is no query), delta
   DocSpan span;
   int first, kv, tile;
-  if (!head_tile(a.s.n_kv_heads, a.tiles, &kv, &tile) || !doc_tile(a.s.k_off, a.s.n_docs, a.s.k_tokens, 64, tile, &span, &first)) return;
+  if (!head_tile(a.s.n_kv_heads, a.tiles, &kv, &tile) || !doc_tile(a.s.k_off, a.s.n_docs, a.s.k_tokens, K::OWN, tile, &span, &first)) return;
   const DocSpan queries = other_rows(a.s.q_off, a.s.n_docs, a.s.q_tokens, span);
-  const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4, share = a.s.n_heads / a.s.n_kv_heads;
-  const int row = first + (threadIdx.x >> 6) * 16 + l16;
+  const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), share = a.s.n_heads / a.s.n_kv_heads;
+  const int row = first + (WIDE ? wave * 16 : 0) + l16, b0 = WIDE ? 0 : wave;
+  typename L::Regs nq, nd;
+  float next_ref = 0.f;
+  auto fetch = [&](int head, int q0) {
+    L::fetch(nq, (const T*)a.q + (size_t)head * DH, a.s.q_stride, q0, queries.end);
+    L::fetch(nd, (const T*)a.dout + (size_t)head * DH, a.s.o_stride, q0, queries.end);
+    if (threadIdx.x < 2 * TILE_ROWS) {
+      const int i = q0 + (threadIdx.x & (TILE_ROWS - 1));
+      next_ref = threadIdx.x < TILE_ROWS ? INFINITY : 0.f;
+      if (i < queries.end) next_ref = (threadIdx.x < TILE_ROWS ? a.ref : a.delta)[(size_t)head * a.s.q_tokens + i];
+    }
+  };
+  const bool some = queries.first < queries.end;
+  if (some) fetch(kv * share, queries.first);
   typename O::Frag k[KS], v[KS];
   own_rows<T, DH>(k, (const T*)a.k + (size_t)kv * DH, a.s.k_stride, row, span.end);
   own_rows<T, DH>(v, (const T*)a.v + (size_t)kv * DH, a.s.v_stride, row, span.end);
@@ -256,54 +345,56 @@ __global__ __launch_bounds__(256) void packed_attention_dkv_kernel(AttnArgs a) {
 #pragma unroll
   for (int d = 0; d < DB; ++d) dk[d] = dv[d] = f32x4{0.f, 0.f, 0.f, 0.f};
   const float unit = a.scale * LOG2E;
-  for (int head = kv * share; head < (kv + 1) * share; ++head) {
-    const T *q = (const T*)a.q + (size_t)head * DH, *dout = (const T*)a.dout + (size_t)head * DH;
-    for (int q0 = queries.first; q0 < queries.end; q0 += TILE_ROWS) {
-      __syncthreads();
-      L::stage(lds, q, a.s.q_stride, q0, queries.end);
-      L::stage(lds + L::BYTES, dout, a.s.o_stride, q0, queries.end);
-      if (threadIdx.x < TILE_ROWS) {
-        const int i = q0 + threadIdx.x;
-        const size_t at = (size_t)head * a.s.q_tokens + i;
-        refs[threadIdx.x] = i < queries.end ? a.ref[at] : INFINITY;
-        refs[TILE_ROWS + threadIdx.x] = i < queries.end ? a.delta[at] : 0.f;
-      }
-      __syncthreads();
-      f32x4 p[4], ds[4];
+  int head = kv * share, q0 = queries.first;
+  while (some && head < (kv + 1) * share) {
+    __syncthreads();
+    L::put(lds, nq);
+    L::put(lds + L::BYTES, nd);
+    if (threadIdx.x < 2 * TILE_ROWS) refs[threadIdx.x] = next_ref;
+    __syncthreads();
+    q0 += TILE_ROWS;
+    if (q0 >= queries.end) {
+      q0 = queries.first;
+      ++head;
+    }
+    if (head < (kv + 1) * share) fetch(head, q0);
+    f32x4 p[NB], ds[NB];
 #pragma unroll
-      for (int b = 0; b < 4; ++b) {
-        f32x4 s = {0.f, 0.f, 0.f, 0.f}, dp = {0.f, 0.f, 0.f, 0.f};
+    for (int b = 0; b < NB; ++b) p[b] = ds[b] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          s = O::mma(L::rows(lds, b, ks), k[ks], s);
-          dp = O::mma(L::rows(lds + L::BYTES, b, ks), v[ks], dp);
-        }
-        const f32x4 ref = *reinterpret_cast<const f32x4*>(refs + b * 16 + 4 * g), delta = *reinterpret_cast<const f32x4*>(refs + TILE_ROWS + b * 16 + 4 * g);
+    for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          p[b][r] = __builtin_amdgcn_exp2f(fmaf(s[r], unit, -ref[r]));
-          ds[b][r] = p[b][r] * (dp[r] - delta[r]);
-        }
+      for (int b = 0; b < NB; ++b) {
+        p[b] = O::mma(L::rows(lds, b0 + b, ks), k[ks], p[b]);
+        ds[b] = O::mma(L::rows(lds + L::BYTES, b0 + b, ks), v[ks], ds[b]);
       }
 #pragma unroll
-      for (int ks = 0; ks < PS; ++ks) {
-        const typename O::Frag pf = step_of<T>(p, ks), df = step_of<T>(ds, ks);
+    for (int b = 0; b < NB; ++b) {
+      const f32x4 ref = *reinterpret_cast<const f32x4*>(refs + (b0 + b) * 16 + 4 * g), delta = *reinterpret_cast<const f32x4*>(refs + TILE_ROWS + (b0 + b) * 16 + 4 * g);
 #pragma unroll
-        for (int d = 0; d < DB; ++d) {
-          dv[d] = O::mma(L::cols(lds + L::BYTES, ks, d), pf, dv[d]);
-          dk[d] = O::mma(L::cols(lds, ks, d), df, dk[d]);
-        }
+      for (int r = 0; r < 4; ++r) {
+        p[b][r] = __builtin_amdgcn_exp2f(fmaf(p[b][r], unit, -ref[r]));
+        ds[b][r] = p[b][r] * (ds[b][r] - delta[r]);
+      }
+    }
+#pragma unroll
+    for (int ks = 0; ks < PS; ++ks) {
+      const typename O::Frag pf = step_of<T>(p, ks), df = step_of<T>(ds, ks);
+#pragma unroll
+      for (int d = 0; d < DB; ++d) {
+        dv[d] = O::mma(L::cols(lds + L::BYTES, b0 + ks, d), pf, dv[d]);
+        dk[d] = O::mma(L::cols(lds, b0 + ks, d), df, dk[d]);
       }
     }
   }
-  if (row >= span.end) return;
   T* tk = (T*)a.dk + (size_t)row * a.s.dk_stride + (size_t)kv * DH + 4 * g;
   T* tv = (T*)a.dv + (size_t)row * a.s.dv_stride + (size_t)kv * DH + 4 * g;
-#pragma unroll
-  for (int d = 0; d < DB; ++d) {
-    store4(tk + 16 * d, dk[d][0] * a.scale, dk[d][1] * a.scale, dk[d][2] * a.scale, dk[d][3] * a.scale);
-    store4(tv + 16 * d, dv[d][0], dv[d][1], dv[d][2], dv[d][3]);
-  }
+  joined<DB, WIDE>(lds, dk, [&](int d, f32x4 x) {
+    if (row < span.end) store4(tk + 16 * d, x[0] * a.scale, x[1] * a.scale, x[2] * a.scale, x[3] * a.scale);
+  });
+  joined<DB, WIDE>(lds, dv, [&](int d, f32x4 x) {
+    if (row < span.end) store4(tv + 16 * d, x[0], x[1], x[2], x[3]);
+  });
 }
 
 static AttnArgs attn_args(const br_attn_shape& s) {
@@ -313,19 +404,23 @@ static AttnArgs attn_args(const br_attn_shape& s) {
   return a;
 }
 
-// f(T, DH)
+// f(T, DH, WIDE); rows x heads: own rows of the launch.  fp32: 64 own rows a workgroup where that gives two workgroups a compute unit, else 16.
 template <typename F>
-static void attn_form(const br_attn_shape& s, F f) {
+static void attn_form(const br_attn_shape& s, long long rows_heads, F f) {
 #define BR_D(n) std::integral_constant<int, n>{}
   if (s.dtype == BR_BF16) {
-    if (s.head_dim == 64) f(bf16{}, BR_D(64));
-    else f(bf16{}, BR_D(128));
-  } else {
-    if (s.head_dim == 16) f(float{}, BR_D(16));
-    else if (s.head_dim == 32) f(float{}, BR_D(32));
-    else if (s.head_dim == 64) f(float{}, BR_D(64));
-    else f(float{}, BR_D(128));
+    if (s.head_dim == 64) f(bf16{}, BR_D(64), std::true_type{});
+    else f(bf16{}, BR_D(128), std::true_type{});
+    return;
   }
+  auto with = [&](auto D) {
+    if (rows_heads >= 2LL * 64 * device_cu_count()) f(float{}, D, std::true_type{});
+    else f(float{}, D, std::false_type{});
+  };
+  if (s.head_dim == 16) with(BR_D(16));
+  else if (s.head_dim == 32) with(BR_D(32));
+  else if (s.head_dim == 64) with(BR_D(64));
+  else with(BR_D(128));
 #undef BR_D
 }
 
@@ -338,11 +433,17 @@ br_status launch_attn_train_forward(const br_attn_shape& s, const void* q, const
   a.v = v;
   a.o = out;
   a.lse = lse;
-  a.tiles = (int)doc_tiles_most(s.n_docs, s.q_tokens, 64);
-  const long long blocks = head_tile_blocks(s.n_heads, a.tiles);
-  BR_REQUIRE(blocks < 0x7FFFFFFFLL, BR_ESHAPE, "br_attention_forward: too many workgroups for one launch");
   if (attn_packed_bf16_fits(s)) return launch_attn_forward_bf16(a, st);
-  attn_form(s, [&](auto Tc, auto Dc) { hipLaunchKernelGGL((packed_attention_kernel<decltype(Tc), decltype(Dc)::value>), dim3((unsigned)blocks), dim3(256), 0, st, a); });
+  br_status ok = BR_OK;
+  attn_form(s, (long long)s.q_tokens * s.n_heads, [&](auto Tc, auto Dc, auto Wc) {
+    using T = decltype(Tc);
+    constexpr int DH = decltype(Dc)::value;
+    constexpr bool WIDE = decltype(Wc)::value;
+    unsigned n;
+    if ((ok = attn_grid(a, s.q_tokens, s.n_heads, Kernel<T, DH, WIDE>::OWN, &n)) != BR_OK) return;
+    hipLaunchKernelGGL((packed_attention_kernel<T, DH, WIDE>), dim3(n), dim3(256), 0, st, a);
+  });
+  if (ok != BR_OK) return ok;
   BR_LAUNCH_CHECK();
   return BR_OK;
 }
@@ -361,18 +462,29 @@ br_status launch_attn_train_backward(const br_attn_shape& s, const void* dout, c
   a.dq = dq;
   a.dk = dk;
   a.dv = dv;
-  const int tq = (int)doc_tiles_most(s.n_docs, s.q_tokens, 64), tk = (int)doc_tiles_most(s.n_docs, s.k_tokens, 64);
-  const long long bq = head_tile_blocks(s.n_heads, tq), bk = head_tile_blocks(s.n_kv_heads, tk);
-  BR_REQUIRE(bq < 0x7FFFFFFFLL && bk < 0x7FFFFFFFLL, BR_ESHAPE, "br_attention_backward: too many workgroups for one launch");
   if (attn_packed_bf16_fits(s)) return launch_attn_grad_bf16(a, st);
-  attn_form(s, [&](auto Tc, auto Dc) {
-    using T = decltype(Tc);
-    constexpr int DH = decltype(Dc)::value;
-    a.tiles = tq;
-    if (s.q_tokens > 0) hipLaunchKernelGGL((packed_attention_dq_kernel<T, DH>), dim3((unsigned)bq), dim3(256), 0, st, a);
-    a.tiles = tk;
-    if (s.k_tokens > 0) hipLaunchKernelGGL((packed_attention_dkv_kernel<T, DH>), dim3((unsigned)bk), dim3(256), 0, st, a);
-  });
+  br_status ok = BR_OK;
+  if (s.q_tokens > 0)
+    attn_form(s, (long long)s.q_tokens * s.n_heads, [&](auto Tc, auto Dc, auto Wc) {
+      using T = decltype(Tc);
+      constexpr int DH = decltype(Dc)::value;
+      constexpr bool WIDE = decltype(Wc)::value;
+      unsigned n;
+      if ((ok = attn_grid(a, s.q_tokens, s.n_heads, Kernel<T, DH, WIDE>::OWN, &n)) != BR_OK) return;
+      hipLaunchKernelGGL((packed_attention_dq_kernel<T, DH, WIDE>), dim3(n), dim3(256), 0, st, a);
+    });
+  if (ok != BR_OK) return ok;
+  BR_LAUNCH_CHECK();
+  if (s.k_tokens > 0)
+    attn_form(s, (long long)s.k_tokens * s.n_kv_heads, [&](auto Tc, auto Dc, auto Wc) {
+      using T = decltype(Tc);
+      constexpr int DH = decltype(Dc)::value;
+      constexpr bool WIDE = decltype(Wc)::value;
+      unsigned n;
+      if ((ok = attn_grid(a, s.k_tokens, s.n_kv_heads, Kernel<T, DH, WIDE>::OWN, &n)) != BR_OK) return;
+      hipLaunchKernelGGL((packed_attention_dkv_kernel<T, DH, WIDE>), dim3(n), dim3(256), 0, st, a);
+    });
+  if (ok != BR_OK) return ok;
   BR_LAUNCH_CHECK();
   return BR_OK;
 }

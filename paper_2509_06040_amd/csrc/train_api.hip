@@ -21,7 +21,7 @@ static br_status attn_check(const br_attn_shape* s, const char* who, bool backwa
   BR_REQUIRE(s->scale >= 0.f && isfinite(s->scale), BR_EINVAL, w + ": scale must be finite and not negative");
   const int d = s->head_dim;
   BR_REQUIRE(d == 64 || d == 128 || (s->dtype == BR_F32 && (d == 16 || d == 32)), BR_ESHAPE, w + ": head_dim must be 64 or 128 (fp32: 16, 32 too)");
-  BR_REQUIRE(s->n_heads <= 65535 && s->n_docs <= (1 << 24), BR_ESHAPE, w + ": too many heads or documents");
+  BR_REQUIRE(s->n_heads <= 65535 && s->n_docs <= (1 << 24) && s->q_tokens <= 0x7FFFFF00 && s->k_tokens <= 0x7FFFFF00, BR_ESHAPE, w + ": too many heads, documents or tokens");
   const int64_t nq = (int64_t)s->n_heads * d, nk = (int64_t)s->n_kv_heads * d, unit = s->dtype == BR_BF16 ? 8 : 4;
   auto stride = [&](int64_t v, int64_t least) { return v >= least && v % unit == 0 && v < (1LL << 31); };
   BR_REQUIRE(stride(s->q_stride, nq) && stride(s->o_stride, nq) && stride(s->k_stride, nk) && stride(s->v_stride, nk), BR_ESHAPE,
@@ -67,7 +67,7 @@ static br_status norm_check(const br_norm_shape* s, const char* who) {
   BR_REQUIRE(s->rows >= 0 && s->n_docs >= 0 && s->n_groups >= 1 && s->hidden >= 4, BR_EINVAL, w + ": bad sizes");
   BR_REQUIRE(s->row_off && (s->n_docs == 0 || s->group), BR_EINVAL, w + ": NULL offsets or groups");
   BR_REQUIRE(s->hidden % 4 == 0 && s->mods_stride % 4 == 0 && s->shift_off % 4 == 0 && s->scale_off % 4 == 0, BR_ESHAPE, w + ": hidden, mods_stride and offsets must be multiples of 4");
-  BR_REQUIRE(s->hidden <= 16384 && s->n_docs <= (1 << 24) && s->n_groups <= 65535, BR_ESHAPE, w + ": hidden above 16384, or too many documents or groups");
+  BR_REQUIRE(s->hidden <= 16384 && s->n_docs <= (1 << 24) && s->n_groups <= 65535 && s->rows <= 0x7FFFFF00, BR_ESHAPE, w + ": hidden above 16384, or too many documents, groups or rows");
   BR_REQUIRE(s->shift_off >= 0 && s->scale_off >= 0 && (int64_t)s->shift_off + s->hidden <= s->mods_stride && (int64_t)s->scale_off + s->hidden <= s->mods_stride, BR_EINVAL,
              w + ": shift and scale must lie within a group's vectors");
   return BR_OK;
