@@ -1,5 +1,7 @@
 // What the kernels of attention over packed documents share: arguments, the rows of a workgroup, operands.
 #pragma once
+#include <algorithm>
+
 #include "dit.h"
 #include "docs.h"
 #include "train.h"
@@ -21,6 +23,11 @@ struct AttnArgs {
   const void *q, *k, *v, *out, *dout;
   float *lse, *ref, *delta;  // ref: lse in powers of two, infinite for a query without keys (its probabilities are zero); delta: dout . out
   void *o, *dq, *dk, *dv;
+  // Launches of few own rows cut the other side's rows of each document in `parts`, a workgroup each, whose sums (fp32, as they stand) a launch behind joins.
+  int parts;
+  unsigned blocks;       // workgroups of a part
+  float *part, *part2;   // [parts][tokens][heads][head_dim]: o, dq or dk; dv
+  float *part_ref, *part_sum;  // forward: [parts][heads][tokens]
 };
 
 __device__ inline float quarters_max(float x) {
@@ -38,6 +45,16 @@ __device__ inline DocSpan other_rows(const int* off, int n, int rows, const DocS
   if (span.doc >= 0) o = doc_item(off, n, rows, span.doc + 1);
   return o;
 }
+// This workgroup's part of them, in whole tiles.
+__device__ inline void take_part(DocSpan* rows, int parts, int part, int tile) {
+  if (parts == 1) return;
+  const long long each = (((long long)rows->end - rows->first + tile - 1) / tile + parts - 1) / parts * tile;
+  const int end = rows->end;
+  rows->first = (int)min<long long>(rows->first + part * each, end);
+  rows->end = (int)min<long long>(rows->first + each, end);
+}
+template <typename T>
+__device__ inline T* part_row(T* base, int part, int tokens, int row, int heads, int head, int dh) { return base + (((size_t)part * tokens + row) * heads + head) * dh; }
 
 // Workgroup -> (head, tile of the head).  Workgroups go round-robin over the 8 XCDs: g = gcd(heads, 8) heads are in work at a time, each on 8 / g XCDs, so
 // that the tiles of a document's head find what they share in their XCD's L2.
@@ -46,26 +63,57 @@ __host__ __device__ inline long long head_tile_blocks(int heads, int tiles) {
   const int g = heads_at_a_time(heads), each = (tiles + 8 / g - 1) / (8 / g);
   return (long long)heads / g * each * 8;
 }
-__device__ inline bool head_tile(int heads, int tiles, int* head, int* tile) {
-  const int g = heads_at_a_time(heads), dies = 8 / g, each = (tiles + dies - 1) / dies, x = blockIdx.x & 7, t = blockIdx.x >> 3;
+__device__ inline bool head_tile(const AttnArgs& a, int heads, int* head, int* tile, int* part) {
+  *part = a.parts == 1 ? 0 : blockIdx.x / a.blocks;
+  const unsigned block = blockIdx.x - *part * a.blocks;  // (a part's workgroups are a multiple of 8)
+  const int tiles = a.tiles, g = heads_at_a_time(heads), dies = 8 / g, each = (tiles + dies - 1) / dies, x = block & 7, t = block >> 3;
   *head = t / each * g + x % g;
   *tile = (t - t / each * each) * dies + x / g;
   return *tile < tiles;
 }
 
-// Tiles of `rows` own rows over all heads: sets a.tiles; workgroups of the launch.
-inline br_status attn_grid(AttnArgs& a, int tokens, int heads, int rows, unsigned* blocks) {
+// Tiles of `rows` own rows over all heads, in `parts`: sets a.tiles, a.parts, a.blocks; workgroups of the launch.
+inline br_status attn_grid(AttnArgs& a, int tokens, int heads, int rows, int parts, unsigned* blocks) {
   const long long tiles = doc_tiles_most(a.s.n_docs, tokens, rows);
   a.tiles = (int)tiles;
+  a.parts = parts;
   const long long n = tiles < 0x7FFFFFFFLL ? head_tile_blocks(heads, a.tiles) : 0x7FFFFFFFLL;
-  BR_REQUIRE(n < 0x7FFFFFFFLL, BR_ESHAPE, "attention: too many workgroups for one launch");
-  *blocks = (unsigned)n;
+  BR_REQUIRE(n * parts < 0x7FFFFFFFLL, BR_ESHAPE, "attention: too many workgroups for one launch");
+  a.blocks = (unsigned)n;
+  *blocks = (unsigned)(n * parts);
   return BR_OK;
+}
+
+// Parts of a launch whose own rows make fewer workgroups than the units take at once (`per_cu` each).  They save the time of the steps that others take (step_us for 32
+// rows of an average document, `heads` times over for keys that several heads of queries share) and cost the join: 4 us, and `outputs` fp32 values of every
+// own row's channel written and read by each part (3 TB/s together).  us in one part / as many as this rule gives, heads of 64 in bf16: 20 queries on 1800 keys, 8
+// heads on two over two documents of 750, see the launchers.
+inline int attn_parts(const br_attn_shape& s, long long own_tokens, int own_heads, int own_rows, long long other_tokens, int heads, int per_cu, float step_us, int outputs) {
+  if (own_tokens == 0 || other_tokens == 0 || s.n_docs == 0) return 1;
+  const long long blocks = std::max<long long>(cdiv(own_tokens, own_rows), std::min<long long>(s.n_docs, own_tokens)) * own_heads;
+  const int tiles = cdiv(cdiv(other_tokens, s.n_docs), 32), most = (int)std::min<long long>({(long long)per_cu * device_cu_count() / blocks, (long long)heads * tiles / 4, tiles, 64});
+  int best = 1;
+  float gain = 3.f;
+  for (int n = 2; n <= most; ++n) {
+    const float g = (float)heads * tiles * step_us * (1.f - 1.f / n) - 4.f - (float)n * own_tokens * own_heads * s.head_dim * outputs * 8.f / 3e6f;
+    if (g > gain) {
+      gain = g;
+      best = n;
+    }
+  }
+  return best;
 }
 
 // ---- attn_packed_bf16.hip
 bool attn_packed_bf16_fits(const br_attn_shape& s);
-br_status launch_attn_forward_bf16(AttnArgs a, hipStream_t st);
-br_status launch_attn_grad_bf16(AttnArgs a, hipStream_t st);
+br_status launch_attn_forward_bf16(AttnArgs a, int parts, hipStream_t st);
+br_status launch_attn_grad_bf16(AttnArgs a, int parts_q, int parts_k, hipStream_t st);
+// ---- attn_train.hip: what the parts leave, into the outputs
+br_status launch_attn_join_forward(const AttnArgs& a, hipStream_t st);
+br_status launch_attn_join_dq(const AttnArgs& a, hipStream_t st);
+br_status launch_attn_join_dkv(const AttnArgs& a, hipStream_t st);
+// own rows of a workgroup and workgroups a unit of the bf16 kernels: forward, dq, dk and dv
+constexpr int PACK_OWN = 128;
+inline int pack_per_cu(int head_dim, int pass) { return head_dim == 128 ? (pass == 2 ? 1 : 2) : pass == 2 ? 2 : 3; }
 
 }  // namespace br

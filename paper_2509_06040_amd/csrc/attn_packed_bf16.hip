@@ -16,13 +16,13 @@ namespace br {
 
 extern __shared__ __attribute__((aligned(1024))) char g_packed_tiles[];
 
-constexpr int PACK_TILE = 32, PACK_OWN = 128;  // rows of a tile, own rows of a workgroup
+constexpr int PACK_TILE = 32;  // rows of a tile
 
 // Waves a SIMD, buffers, and tiles between two barriers.
 enum class Pass { FORWARD, QUERIES, KEYS };
 template <int DH, Pass PASS>
 struct PackForm {
-  static constexpr int WPE = DH == 128 ? (PASS == Pass::KEYS ? 1 : 2) : PASS == Pass::KEYS ? 2 : 3;
+  static constexpr int WPE = DH == 128 ? (PASS == Pass::KEYS ? 1 : 2) : PASS == Pass::KEYS ? 2 : 3;  // (pack_per_cu)
   static constexpr int NB = DH == 128 ? (PASS == Pass::KEYS ? 6 : 4) : 6, EACH = NB >= 6 ? 2 : 1;
   static constexpr int LDS = NB * (2 * PACK_TILE * DH * 2 + (PASS == Pass::KEYS ? 2 * PACK_TILE * 4 : 0));
 };
@@ -139,10 +139,11 @@ __global__ __launch_bounds__(256, (PackForm<DH, Pass::FORWARD>::WPE)) void packe
   static_assert(NS % FR == 0 && NB % 2 == 0 && NB % EACH == 0 && NB >= 2 + 2 * EACH, "");
   char* lds = g_packed_tiles;
   const int share = a.s.n_heads / a.s.n_kv_heads;
-  int head, tile, own0;
+  int head, tile, part_of, own0;
   DocSpan own;
-  if (!head_tile(a.s.n_heads, a.tiles, &head, &tile) || !doc_tile(a.s.q_off, a.s.n_docs, a.s.q_tokens, PACK_OWN, tile, &own, &own0)) return;
-  const DocSpan keys = other_rows(a.s.k_off, a.s.n_docs, a.s.k_tokens, own);
+  if (!head_tile(a, a.s.n_heads, &head, &tile, &part_of) || !doc_tile(a.s.q_off, a.s.n_docs, a.s.q_tokens, PACK_OWN, tile, &own, &own0)) return;
+  DocSpan keys = other_rows(a.s.k_off, a.s.n_docs, a.s.k_tokens, own);
+  take_part(&keys, a.parts, part_of, PACK_TILE);
   const int kv = head / share, lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4;
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row0 = own0 + wv * 32;
   const bool active = row0 < own.end;  // (uniform over the wave)
@@ -301,6 +302,17 @@ __global__ __launch_bounds__(256, (PackForm<DH, Pass::FORWARD>::WPE)) void packe
     const float total = quarters_sum(sum[qb]), inv = total == 0.f ? 0.f : 1.f / total;
     const int row = row0 + qb * 16 + l16;
     if (row >= own.end) continue;
+    if (a.parts > 1) {
+      float* to = part_row(a.part, part_of, a.s.q_tokens, row, a.s.n_heads, head, DH) + 4 * g;
+#pragma unroll
+      for (int d = 0; d < DB; ++d) *reinterpret_cast<f32x4*>(to + 16 * d) = o[d][qb];
+      if (g == 0) {
+        const size_t at = ((size_t)part_of * a.s.n_heads + head) * a.s.q_tokens + row;
+        a.part_ref[at] = ref[qb];
+        a.part_sum[at] = total;
+      }
+      continue;
+    }
     bf16* out = (bf16*)a.o + (size_t)row * a.s.o_stride + (size_t)head * DH + 4 * g;
 #pragma unroll
     for (int d = 0; d < DB; ++d) store4(out + 16 * d, o[d][qb][0] * inv, o[d][qb][1] * inv, o[d][qb][2] * inv, o[d][qb][3] * inv);
@@ -322,13 +334,14 @@ __global__ __launch_bounds__(256, (PackForm<DH, PASS>::WPE)) void packed_grad_bf
   char* lds = g_packed_tiles;
 
   const int share = a.s.n_heads / a.s.n_kv_heads;
-  int head, tile, own0;
+  int head, tile, part_of, own0;
   DocSpan own;
   const int* own_off = KEYS ? a.s.k_off : a.s.q_off;
-  if (!head_tile(KEYS ? a.s.n_kv_heads : a.s.n_heads, a.tiles, &head, &tile) ||
+  if (!head_tile(a, KEYS ? a.s.n_kv_heads : a.s.n_heads, &head, &tile, &part_of) ||
       !doc_tile(own_off, a.s.n_docs, KEYS ? a.s.k_tokens : a.s.q_tokens, PACK_OWN, tile, &own, &own0))
     return;
-  const DocSpan other = other_rows(KEYS ? a.s.q_off : a.s.k_off, a.s.n_docs, KEYS ? a.s.q_tokens : a.s.k_tokens, own);
+  DocSpan other = other_rows(KEYS ? a.s.q_off : a.s.k_off, a.s.n_docs, KEYS ? a.s.q_tokens : a.s.k_tokens, own);
+  take_part(&other, a.parts, part_of, PACK_TILE);
   const int kv = KEYS ? head : head / share, h0 = KEYS ? head * share : head;
   const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g = lane >> 4;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -361,7 +374,7 @@ __global__ __launch_bounds__(256, (PackForm<DH, PASS>::WPE)) void packed_grad_bf
       const float lse = a.lse[at];
       delta[qb] = quarters_sum(d);
       ref[qb] = lse == -INFINITY ? INFINITY : lse * LOG2E;
-      if (g == 0 && row0 + qb * 16 + l16 < own.end) {
+      if (g == 0 && row0 + qb * 16 + l16 < own.end && part_of == 0) {
         a.ref[at] = ref[qb];
         a.delta[at] = delta[qb];
       }
@@ -530,6 +543,18 @@ __global__ __launch_bounds__(256, (PackForm<DH, PASS>::WPE)) void packed_grad_bf
   for (int qb = 0; qb < QB; ++qb) {
     const int row = row0 + qb * 16 + l16;
     if (row >= own.end) continue;
+    if (a.parts > 1) {
+      const int tokens = KEYS ? a.s.k_tokens : a.s.q_tokens, heads = KEYS ? a.s.n_kv_heads : a.s.n_heads;
+      float* to = part_row(a.part, part_of, tokens, row, heads, head, DH) + 4 * g;
+#pragma unroll
+      for (int d = 0; d < DB; ++d) *reinterpret_cast<f32x4*>(to + 16 * d) = acc1[d][qb];
+      if constexpr (KEYS) {
+        to = part_row(a.part2, part_of, tokens, row, heads, head, DH) + 4 * g;
+#pragma unroll
+        for (int d = 0; d < DB; ++d) *reinterpret_cast<f32x4*>(to + 16 * d) = acc2[d][qb];
+      }
+      continue;
+    }
     bf16* to1 = KEYS ? (bf16*)a.dk + (size_t)row * a.s.dk_stride + (size_t)kv * DH + 4 * g : (bf16*)a.dq + (size_t)row * a.s.dq_stride + (size_t)head * DH + 4 * g;
 #pragma unroll
     for (int d = 0; d < DB; ++d) store4(to1 + 16 * d, acc1[d][qb][0] * a.scale, acc1[d][qb][1] * a.scale, acc1[d][qb][2] * a.scale, acc1[d][qb][3] * a.scale);
@@ -541,41 +566,44 @@ __global__ __launch_bounds__(256, (PackForm<DH, PASS>::WPE)) void packed_grad_bf
   }
 }
 
+br_status launch_attn_forward_bf16(AttnArgs a, int parts, hipStream_t st) {
+  unsigned n;
+  const br_status ok = attn_grid(a, a.s.q_tokens, a.s.n_heads, PACK_OWN, parts, &n);
+  if (ok != BR_OK) return ok;
+  if (a.s.head_dim == 64) hipLaunchKernelGGL((packed_forward_bf16_kernel<64>), dim3(n), dim3(256), (PackForm<64, Pass::FORWARD>::LDS), st, a);
+  else hipLaunchKernelGGL((packed_forward_bf16_kernel<128>), dim3(n), dim3(256), (PackForm<128, Pass::FORWARD>::LDS), st, a);
+  BR_LAUNCH_CHECK();
+  return parts > 1 ? launch_attn_join_forward(a, st) : BR_OK;
+}
+
+template <int DH>
+static br_status grad_launch(AttnArgs a, int parts_q, int parts_k, hipStream_t st) {
+  unsigned n;
+  if (a.s.q_tokens > 0) {
+    br_status ok = attn_grid(a, a.s.q_tokens, a.s.n_heads, PACK_OWN, parts_q, &n);
+    if (ok != BR_OK) return ok;
+    hipLaunchKernelGGL((packed_grad_bf16_kernel<DH, Pass::QUERIES>), dim3(n), dim3(256), (PackForm<DH, Pass::QUERIES>::LDS), st, a);
+    BR_LAUNCH_CHECK();
+    if (parts_q > 1 && (ok = launch_attn_join_dq(a, st)) != BR_OK) return ok;
+  }
+  if (a.s.k_tokens > 0) {
+    br_status ok = attn_grid(a, a.s.k_tokens, a.s.n_kv_heads, PACK_OWN, parts_k, &n);
+    if (ok != BR_OK) return ok;
+    hipLaunchKernelGGL((packed_grad_bf16_kernel<DH, Pass::KEYS>), dim3(n), dim3(256), (PackForm<DH, Pass::KEYS>::LDS), st, a);
+    BR_LAUNCH_CHECK();
+    if (parts_k > 1 && (ok = launch_attn_join_dkv(a, st)) != BR_OK) return ok;
+  }
+  return BR_OK;
+}
+
+br_status launch_attn_grad_bf16(AttnArgs a, int parts_q, int parts_k, hipStream_t st) {
+  return a.s.head_dim == 64 ? grad_launch<64>(a, parts_q, parts_k, st) : grad_launch<128>(a, parts_q, parts_k, st);
+}
+
 // Rows of a document are addressed with 32-bit byte offsets from its first one.
 bool attn_packed_bf16_fits(const br_attn_shape& s) {
   auto fits = [](int64_t tokens, int64_t stride) { return tokens * stride * 2 < (1LL << 32); };
   return s.dtype == BR_BF16 && fits(s.q_tokens, s.q_stride) && fits(s.q_tokens, s.o_stride) && fits(s.k_tokens, s.k_stride) && fits(s.k_tokens, s.v_stride);
 }
-
-br_status launch_attn_forward_bf16(AttnArgs a, hipStream_t st) {
-  unsigned n;
-  const br_status ok = attn_grid(a, a.s.q_tokens, a.s.n_heads, PACK_OWN, &n);
-  if (ok != BR_OK) return ok;
-  const dim3 grid(n);
-  if (a.s.head_dim == 64) hipLaunchKernelGGL((packed_forward_bf16_kernel<64>), grid, dim3(256), (PackForm<64, Pass::FORWARD>::LDS), st, a);
-  else hipLaunchKernelGGL((packed_forward_bf16_kernel<128>), grid, dim3(256), (PackForm<128, Pass::FORWARD>::LDS), st, a);
-  BR_LAUNCH_CHECK();
-  return BR_OK;
-}
-
-template <int DH>
-static br_status grad_launch(AttnArgs a, hipStream_t st) {
-  unsigned n;
-  if (a.s.q_tokens > 0) {
-    const br_status ok = attn_grid(a, a.s.q_tokens, a.s.n_heads, PACK_OWN, &n);
-    if (ok != BR_OK) return ok;
-    hipLaunchKernelGGL((packed_grad_bf16_kernel<DH, Pass::QUERIES>), dim3(n), dim3(256), (PackForm<DH, Pass::QUERIES>::LDS), st, a);
-    BR_LAUNCH_CHECK();
-  }
-  if (a.s.k_tokens > 0) {
-    const br_status ok = attn_grid(a, a.s.k_tokens, a.s.n_kv_heads, PACK_OWN, &n);
-    if (ok != BR_OK) return ok;
-    hipLaunchKernelGGL((packed_grad_bf16_kernel<DH, Pass::KEYS>), dim3(n), dim3(256), (PackForm<DH, Pass::KEYS>::LDS), st, a);
-    BR_LAUNCH_CHECK();
-  }
-  return BR_OK;
-}
-
-br_status launch_attn_grad_bf16(AttnArgs a, hipStream_t st) { return a.s.head_dim == 64 ? grad_launch<64>(a, st) : grad_launch<128>(a, st); }
 
 }  // namespace br

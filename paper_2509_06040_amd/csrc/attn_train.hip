@@ -146,9 +146,10 @@ __global__ __launch_bounds__(256) void packed_attention_kernel(AttnArgs a) {
   __shared__ __attribute__((aligned(16))) char lds[2 * L::BYTES];
   __shared__ float tops[4][16], sums[4][16];
   DocSpan span;
-  int first, head, tile;
-  if (!head_tile(a.s.n_heads, a.tiles, &head, &tile) || !doc_tile(a.s.q_off, a.s.n_docs, a.s.q_tokens, K::OWN, tile, &span, &first)) return;
-  const DocSpan keys = other_rows(a.s.k_off, a.s.n_docs, a.s.k_tokens, span);
+  int first, head, tile, part_of;
+  if (!head_tile(a, a.s.n_heads, &head, &tile, &part_of) || !doc_tile(a.s.q_off, a.s.n_docs, a.s.q_tokens, K::OWN, tile, &span, &first)) return;
+  DocSpan keys = other_rows(a.s.k_off, a.s.n_docs, a.s.k_tokens, span);
+  take_part(&keys, a.parts, part_of, TILE_ROWS);
   const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), kv = head / (a.s.n_heads / a.s.n_kv_heads);
   const int row = first + (WIDE ? wave * 16 : 0) + l16, b0 = WIDE ? 0 : wave;
   const T *k = (const T*)a.k + (size_t)kv * DH, *v = (const T*)a.v + (size_t)kv * DH;
@@ -221,6 +222,18 @@ __global__ __launch_bounds__(256) void packed_attention_kernel(AttnArgs a) {
     for (int w = 0; w < 4; ++w) sum += sums[w][l16] * __builtin_amdgcn_exp2f(tops[w][l16] - ref);
     top = most;
   }
+  if (a.parts > 1) {
+    float* to = part_row(a.part, part_of, a.s.q_tokens, row, a.s.n_heads, head, DH) + 4 * g;
+    joined<DB, WIDE>(lds, o, [&](int d, f32x4 x) {
+      if (row < span.end) *reinterpret_cast<f32x4*>(to + 16 * d) = x;
+    });
+    if (row < span.end && g == 0 && (WIDE || wave == 0)) {
+      const size_t at = ((size_t)part_of * a.s.n_heads + head) * a.s.q_tokens + row;
+      a.part_ref[at] = top;
+      a.part_sum[at] = sum;
+    }
+    return;
+  }
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
   T* out = (T*)a.o + (size_t)row * a.s.o_stride + (size_t)head * DH + 4 * g;
   joined<DB, WIDE>(lds, o, [&](int d, f32x4 x) {
@@ -238,9 +251,10 @@ __global__ __launch_bounds__(256) void packed_attention_dq_kernel(AttnArgs a) {
   constexpr int KS = K::KS, PS = K::PS, DB = K::DB, NB = K::NB;
   __shared__ __attribute__((aligned(16))) char lds[2 * L::BYTES];
   DocSpan span;
-  int first, head, tile;
-  if (!head_tile(a.s.n_heads, a.tiles, &head, &tile) || !doc_tile(a.s.q_off, a.s.n_docs, a.s.q_tokens, K::OWN, tile, &span, &first)) return;
-  const DocSpan keys = other_rows(a.s.k_off, a.s.n_docs, a.s.k_tokens, span);
+  int first, head, tile, part_of;
+  if (!head_tile(a, a.s.n_heads, &head, &tile, &part_of) || !doc_tile(a.s.q_off, a.s.n_docs, a.s.q_tokens, K::OWN, tile, &span, &first)) return;
+  DocSpan keys = other_rows(a.s.k_off, a.s.n_docs, a.s.k_tokens, span);
+  take_part(&keys, a.parts, part_of, TILE_ROWS);
   const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), kv = head / (a.s.n_heads / a.s.n_kv_heads);
   const int row = first + (WIDE ? wave * 16 : 0) + l16, b0 = WIDE ? 0 : wave;
   const T *k = (const T*)a.k + (size_t)kv * DH, *v = (const T*)a.v + (size_t)kv * DH;
@@ -263,7 +277,7 @@ __global__ __launch_bounds__(256) void packed_attention_dq_kernel(AttnArgs a) {
       const size_t at = (size_t)head * a.s.q_tokens + row;
       const float lse = a.lse[at];
       if (lse != -INFINITY) ref = lse * LOG2E;
-      if (g == 0 && (WIDE || wave == 0)) {
+      if (g == 0 && (WIDE || wave == 0) && part_of == 0) {
         a.ref[at] = ref;
         a.delta[at] = delta;
       }
@@ -304,6 +318,13 @@ __global__ __launch_bounds__(256) void packed_attention_dq_kernel(AttnArgs a) {
       for (int d = 0; d < DB; ++d) dq[d] = O::mma(L::cols(lds, b0 + ks, d), f, dq[d]);
     }
   }
+  if (a.parts > 1) {
+    float* to = part_row(a.part, part_of, a.s.q_tokens, row, a.s.n_heads, head, DH) + 4 * g;
+    joined<DB, WIDE>(lds, dq, [&](int d, f32x4 x) {
+      if (row < span.end) *reinterpret_cast<f32x4*>(to + 16 * d) = x;
+    });
+    return;
+  }
   T* to = (T*)a.dq + (size_t)row * a.s.dq_stride + (size_t)head * DH + 4 * g;
   joined<DB, WIDE>(lds, dq, [&](int d, f32x4 x) {
     if (row < span.end) store4(to + 16 * d, x[0] * a.scale, x[1] * a.scale, x[2] * a.scale, x[3] * a.scale);
@@ -320,9 +341,10 @@ __global__ __launch_bounds__(256) void packed_attention_dkv_kernel(AttnArgs a) {
   __shared__ __attribute__((aligned(16))) char lds[2 * L::BYTES];
   __shared__ __attribute__((aligned(16))) float refs[2 * TILE_ROWS];  // ref (infinite where there is no query), delta
   DocSpan span;
-  int first, kv, tile;
-  if (!head_tile(a.s.n_kv_heads, a.tiles, &kv, &tile) || !doc_tile(a.s.k_off, a.s.n_docs, a.s.k_tokens, K::OWN, tile, &span, &first)) return;
-  const DocSpan queries = other_rows(a.s.q_off, a.s.n_docs, a.s.q_tokens, span);
+  int first, kv, tile, part_of;
+  if (!head_tile(a, a.s.n_kv_heads, &kv, &tile, &part_of) || !doc_tile(a.s.k_off, a.s.n_docs, a.s.k_tokens, K::OWN, tile, &span, &first)) return;
+  DocSpan queries = other_rows(a.s.q_off, a.s.n_docs, a.s.q_tokens, span);
+  take_part(&queries, a.parts, part_of, TILE_ROWS);
   const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), share = a.s.n_heads / a.s.n_kv_heads;
   const int row = first + (WIDE ? wave * 16 : 0) + l16, b0 = WIDE ? 0 : wave;
   typename L::Regs nq, nd;
@@ -387,6 +409,17 @@ __global__ __launch_bounds__(256) void packed_attention_dkv_kernel(AttnArgs a) {
       }
     }
   }
+  if (a.parts > 1) {
+    float* pk = part_row(a.part, part_of, a.s.k_tokens, row, a.s.n_kv_heads, kv, DH) + 4 * g;
+    float* pv = part_row(a.part2, part_of, a.s.k_tokens, row, a.s.n_kv_heads, kv, DH) + 4 * g;
+    joined<DB, WIDE>(lds, dk, [&](int d, f32x4 x) {
+      if (row < span.end) *reinterpret_cast<f32x4*>(pk + 16 * d) = x;
+    });
+    joined<DB, WIDE>(lds, dv, [&](int d, f32x4 x) {
+      if (row < span.end) *reinterpret_cast<f32x4*>(pv + 16 * d) = x;
+    });
+    return;
+  }
   T* tk = (T*)a.dk + (size_t)row * a.s.dk_stride + (size_t)kv * DH + 4 * g;
   T* tv = (T*)a.dv + (size_t)row * a.s.dv_stride + (size_t)kv * DH + 4 * g;
   joined<DB, WIDE>(lds, dk, [&](int d, f32x4 x) {
@@ -397,16 +430,100 @@ __global__ __launch_bounds__(256) void packed_attention_dkv_kernel(AttnArgs a) {
   });
 }
 
+// ---- joins of the parts, four channels a thread, in the parts' order
+template <typename T>
+__global__ __launch_bounds__(256) void packed_join_kernel(const float* __restrict__ part, const float* __restrict__ part2, T* __restrict__ to, T* __restrict__ to2, long long stride,
+                                                          long long stride2, int parts, long long quads, int row_quads, float scale, float scale2) {
+  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+  if (i >= quads) return;
+  const bool second = blockIdx.y == 1;
+  const f32x4* p = reinterpret_cast<const f32x4*>(second ? part2 : part) + i;
+  f32x4 x = p[0];
+#pragma unroll 4
+  for (int k = 1; k < parts; ++k) x += p[k * quads];
+  x *= second ? scale2 : scale;
+  store4((second ? to2 : to) + i / row_quads * (second ? stride2 : stride) + i % row_quads * 4, x[0], x[1], x[2], x[3]);
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void packed_join_forward_kernel(AttnArgs a, long long quads) {
+  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+  if (i >= quads) return;
+  const int dq = a.s.head_dim / 4, row_quads = a.s.n_heads * dq, row = (int)(i / row_quads), head = (int)(i % row_quads) / dq;
+  const size_t at = (size_t)head * a.s.q_tokens + row, each = (size_t)a.s.n_heads * a.s.q_tokens;
+  float most = -INFINITY;
+  for (int k = 0; k < a.parts; ++k) most = __builtin_elementwise_maximum(most, a.part_ref[k * each + at]);
+  const float ref = most == -INFINITY ? 0.f : most;
+  const f32x4* p = reinterpret_cast<const f32x4*>(a.part) + i;
+  f32x4 x = {0.f, 0.f, 0.f, 0.f};
+  float sum = 0.f;
+#pragma unroll 4
+  for (int k = 0; k < a.parts; ++k) {
+    const float w = __builtin_amdgcn_exp2f(a.part_ref[k * each + at] - ref);
+    x += p[k * quads] * w;
+    sum += a.part_sum[k * each + at] * w;
+  }
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  store4((T*)a.o + (size_t)row * a.s.o_stride + i % row_quads * 4, x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
+  if (i % dq == 0) a.lse[at] = sum == 0.f ? -INFINITY : (most + __builtin_amdgcn_logf(sum)) * LN2;
+}
+
+br_status launch_attn_join_forward(const AttnArgs& a, hipStream_t st) {
+  const long long quads = (long long)a.s.q_tokens * a.s.n_heads * a.s.head_dim / 4;
+  if (a.s.dtype == BR_BF16) hipLaunchKernelGGL(packed_join_forward_kernel<bf16>, dim3(cdiv(quads, 256)), dim3(256), 0, st, a, quads);
+  else hipLaunchKernelGGL(packed_join_forward_kernel<float>, dim3(cdiv(quads, 256)), dim3(256), 0, st, a, quads);
+  BR_LAUNCH_CHECK();
+  return BR_OK;
+}
+static br_status join(const AttnArgs& a, int tokens, int heads, void* to, void* to2, long long stride, long long stride2, float scale, float scale2, hipStream_t st) {
+  const int row_quads = heads * a.s.head_dim / 4;
+  const long long quads = (long long)tokens * row_quads;
+  const dim3 grid(cdiv(quads, 256), to2 ? 2 : 1);
+  if (a.s.dtype == BR_BF16)
+    hipLaunchKernelGGL(packed_join_kernel<bf16>, grid, dim3(256), 0, st, a.part, a.part2, (bf16*)to, (bf16*)to2, stride, stride2, a.parts, quads, row_quads, scale, scale2);
+  else
+    hipLaunchKernelGGL(packed_join_kernel<float>, grid, dim3(256), 0, st, a.part, a.part2, (float*)to, (float*)to2, stride, stride2, a.parts, quads, row_quads, scale, scale2);
+  BR_LAUNCH_CHECK();
+  return BR_OK;
+}
+br_status launch_attn_join_dq(const AttnArgs& a, hipStream_t st) { return join(a, a.s.q_tokens, a.s.n_heads, a.dq, nullptr, a.s.dq_stride, 0, a.scale, 1.f, st); }
+br_status launch_attn_join_dkv(const AttnArgs& a, hipStream_t st) { return join(a, a.s.k_tokens, a.s.n_kv_heads, a.dk, a.dv, a.s.dk_stride, a.s.dv_stride, a.scale, 1.f, st); }
+
 static AttnArgs attn_args(const br_attn_shape& s) {
   AttnArgs a{};
   a.s = s;
   a.scale = s.scale > 0.f ? s.scale : (float)(1.0 / sqrt((double)s.head_dim));
+  a.parts = 1;
   return a;
 }
 
-// f(T, DH, WIDE); rows x heads: own rows of the launch.  fp32: 64 own rows a workgroup where that gives two workgroups a compute unit, else 16.
+// fp32: 64 own rows a workgroup where that gives one workgroup a compute unit (backward: two), else 16.  us with 64 / 16, heads of 64: forward 7200 own rows over all
+// heads 16.4 / 14.1, 17 600 32.1 / 32.8, 35 200 44.3 / 51.2; backward 17 600 94.5 / 84.9, 35 200 137 / 138, 70 400 224 / 253; heads of 128 the same way.
+static bool attn_f32_wide(long long rows_heads, bool backward) { return rows_heads >= (backward ? 2LL : 1LL) * 64 * device_cu_count(); }
+
+// Parts of the launches of a call.
+struct AttnPlan {
+  int forward, dq, dkv;
+};
+static AttnPlan attn_plan(const br_attn_shape& s) {
+  const int share = s.n_heads / s.n_kv_heads, d = s.head_dim;
+  const bool bf = s.dtype == BR_BF16;
+  if (bf && !attn_packed_bf16_fits(s)) return {1, 1, 1};
+  const long long q = (long long)s.q_tokens * s.n_heads, k = (long long)s.k_tokens * s.n_kv_heads;
+  const int own = bf ? PACK_OWN : 16;
+  // (time of 32 rows of the other side in a workgroup, us)
+  auto queries = [&](bool backward) {
+    if (!bf && attn_f32_wide(q, backward)) return 1;
+    const float step = bf ? (backward ? 0.4f : 0.3f) + 0.0015f * d : d / (backward ? 70.f : 90.f);
+    return attn_parts(s, s.q_tokens, s.n_heads, own, s.k_tokens, 1, bf ? pack_per_cu(d, backward ? 1 : 0) : 2, step, 1);
+  };
+  const int keys = !bf && attn_f32_wide(k, true) ? 1 : attn_parts(s, s.k_tokens, s.n_kv_heads, own, s.q_tokens, share, bf ? pack_per_cu(d, 2) : 2, bf ? 0.4f + 0.005f * d : d / 50.f, 2);
+  return {queries(false), queries(true), keys};
+}
+
+// f(T, DH, WIDE)
 template <typename F>
-static void attn_form(const br_attn_shape& s, long long rows_heads, F f) {
+static void attn_form(const br_attn_shape& s, bool wide, F f) {
 #define BR_D(n) std::integral_constant<int, n>{}
   if (s.dtype == BR_BF16) {
     if (s.head_dim == 64) f(bf16{}, BR_D(64), std::true_type{});
@@ -414,7 +531,7 @@ static void attn_form(const br_attn_shape& s, long long rows_heads, F f) {
     return;
   }
   auto with = [&](auto D) {
-    if (rows_heads >= 2LL * 64 * device_cu_count()) f(float{}, D, std::true_type{});
+    if (wide) f(float{}, D, std::true_type{});
     else f(float{}, D, std::false_type{});
   };
   if (s.head_dim == 16) with(BR_D(16));
@@ -424,68 +541,87 @@ static void attn_form(const br_attn_shape& s, long long rows_heads, F f) {
 #undef BR_D
 }
 
-size_t attn_train_workspace(const br_attn_shape& s, bool backward) { return backward ? 2 * align_up((size_t)s.n_heads * s.q_tokens * 4, 256) : 0; }
+// Workspace: ref and delta of the backward pass, then what the parts of one launch leave.
+static size_t attn_rows_bytes(const br_attn_shape& s) { return align_up((size_t)s.n_heads * s.q_tokens * 4, 256); }
+size_t attn_train_workspace(const br_attn_shape& s, bool backward) {
+  const AttnPlan p = attn_plan(s);
+  const size_t q = align_up((size_t)s.q_tokens * s.n_heads * s.head_dim * 4, 256), k = align_up((size_t)s.k_tokens * s.n_kv_heads * s.head_dim * 4, 256);
+  if (!backward) return p.forward > 1 ? p.forward * (q + 2 * attn_rows_bytes(s)) : 0;
+  return 2 * attn_rows_bytes(s) + std::max(p.dq > 1 ? p.dq * q : 0, p.dkv > 1 ? 2 * p.dkv * k : 0);
+}
 
 br_status launch_attn_train_forward(const br_attn_shape& s, const void* q, const void* k, const void* v, void* out, float* lse, void* ws, hipStream_t st) {
   AttnArgs a = attn_args(s);
+  const AttnPlan plan = attn_plan(s);
   a.q = q;
   a.k = k;
   a.v = v;
   a.o = out;
   a.lse = lse;
-  if (attn_packed_bf16_fits(s)) return launch_attn_forward_bf16(a, st);
+  a.part = reinterpret_cast<float*>(ws);
+  a.part_ref = a.part + (size_t)plan.forward * s.q_tokens * s.n_heads * s.head_dim;
+  a.part_sum = a.part_ref + (size_t)plan.forward * s.q_tokens * s.n_heads;
+  if (attn_packed_bf16_fits(s)) return launch_attn_forward_bf16(a, plan.forward, st);
   br_status ok = BR_OK;
-  attn_form(s, (long long)s.q_tokens * s.n_heads, [&](auto Tc, auto Dc, auto Wc) {
+  attn_form(s, attn_f32_wide((long long)s.q_tokens * s.n_heads, false), [&](auto Tc, auto Dc, auto Wc) {
     using T = decltype(Tc);
     constexpr int DH = decltype(Dc)::value;
     constexpr bool WIDE = decltype(Wc)::value;
     unsigned n;
-    if ((ok = attn_grid(a, s.q_tokens, s.n_heads, Kernel<T, DH, WIDE>::OWN, &n)) != BR_OK) return;
+    if ((ok = attn_grid(a, s.q_tokens, s.n_heads, Kernel<T, DH, WIDE>::OWN, plan.forward, &n)) != BR_OK) return;
     hipLaunchKernelGGL((packed_attention_kernel<T, DH, WIDE>), dim3(n), dim3(256), 0, st, a);
   });
   if (ok != BR_OK) return ok;
   BR_LAUNCH_CHECK();
-  return BR_OK;
+  return plan.forward > 1 ? launch_attn_join_forward(a, st) : BR_OK;
 }
 
 br_status launch_attn_train_backward(const br_attn_shape& s, const void* dout, const void* q, const void* k, const void* v, const void* out, const float* lse, void* dq, void* dk,
                                      void* dv, void* ws, hipStream_t st) {
   AttnArgs a = attn_args(s);
+  const AttnPlan plan = attn_plan(s);
   a.q = q;
   a.k = k;
   a.v = v;
   a.out = out;
   a.dout = dout;
   a.lse = const_cast<float*>(lse);
-  a.ref = reinterpret_cast<float*>(ws);
-  a.delta = reinterpret_cast<float*>(reinterpret_cast<char*>(ws) + align_up((size_t)s.n_heads * s.q_tokens * 4, 256));
+  char* w = reinterpret_cast<char*>(ws);
+  a.ref = reinterpret_cast<float*>(w);
+  a.delta = reinterpret_cast<float*>(w + attn_rows_bytes(s));
+  a.part = reinterpret_cast<float*>(w + 2 * attn_rows_bytes(s));
+  a.part2 = a.part + (size_t)plan.dkv * s.k_tokens * s.n_kv_heads * s.head_dim;
   a.dq = dq;
   a.dk = dk;
   a.dv = dv;
-  if (attn_packed_bf16_fits(s)) return launch_attn_grad_bf16(a, st);
+  if (attn_packed_bf16_fits(s)) return launch_attn_grad_bf16(a, plan.dq, plan.dkv, st);
   br_status ok = BR_OK;
-  if (s.q_tokens > 0)
-    attn_form(s, (long long)s.q_tokens * s.n_heads, [&](auto Tc, auto Dc, auto Wc) {
+  if (s.q_tokens > 0) {
+    attn_form(s, attn_f32_wide((long long)s.q_tokens * s.n_heads, true), [&](auto Tc, auto Dc, auto Wc) {
       using T = decltype(Tc);
       constexpr int DH = decltype(Dc)::value;
       constexpr bool WIDE = decltype(Wc)::value;
       unsigned n;
-      if ((ok = attn_grid(a, s.q_tokens, s.n_heads, Kernel<T, DH, WIDE>::OWN, &n)) != BR_OK) return;
+      if ((ok = attn_grid(a, s.q_tokens, s.n_heads, Kernel<T, DH, WIDE>::OWN, plan.dq, &n)) != BR_OK) return;
       hipLaunchKernelGGL((packed_attention_dq_kernel<T, DH, WIDE>), dim3(n), dim3(256), 0, st, a);
     });
-  if (ok != BR_OK) return ok;
-  BR_LAUNCH_CHECK();
-  if (s.k_tokens > 0)
-    attn_form(s, (long long)s.k_tokens * s.n_kv_heads, [&](auto Tc, auto Dc, auto Wc) {
+    if (ok != BR_OK) return ok;
+    BR_LAUNCH_CHECK();
+    if (plan.dq > 1 && (ok = launch_attn_join_dq(a, st)) != BR_OK) return ok;
+  }
+  if (s.k_tokens > 0) {
+    attn_form(s, attn_f32_wide((long long)s.k_tokens * s.n_kv_heads, true), [&](auto Tc, auto Dc, auto Wc) {
       using T = decltype(Tc);
       constexpr int DH = decltype(Dc)::value;
       constexpr bool WIDE = decltype(Wc)::value;
       unsigned n;
-      if ((ok = attn_grid(a, s.k_tokens, s.n_kv_heads, Kernel<T, DH, WIDE>::OWN, &n)) != BR_OK) return;
+      if ((ok = attn_grid(a, s.k_tokens, s.n_kv_heads, Kernel<T, DH, WIDE>::OWN, plan.dkv, &n)) != BR_OK) return;
       hipLaunchKernelGGL((packed_attention_dkv_kernel<T, DH, WIDE>), dim3(n), dim3(256), 0, st, a);
     });
-  if (ok != BR_OK) return ok;
-  BR_LAUNCH_CHECK();
+    if (ok != BR_OK) return ok;
+    BR_LAUNCH_CHECK();
+    if (plan.dkv > 1 && (ok = launch_attn_join_dkv(a, st)) != BR_OK) return ok;
+  }
   return BR_OK;
 }
 
