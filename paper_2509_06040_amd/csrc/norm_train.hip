@@ -121,8 +121,12 @@ __global__ __launch_bounds__(256) void norm_forward_kernel(br_norm_shape s, int 
 
 // A workgroup takes a tile of consecutive rows of one document, each of its row groups every (256 / TPR)-th of them, and leaves the tile's column sums in
 // part[tile][dout | dout y][H] and its group in tile_group[tile].
+// Workgroups a compute unit that the registers of the backward pass allow.
+template <int VPL, int TPR>
+constexpr int NORM_PER_CU = TPR == 64 ? (VPL <= 1 ? 8 : VPL <= 2 ? 5 : VPL <= 3 ? 4 : VPL <= 4 ? 3 : 2) : VPL <= 3 ? 4 : VPL <= 4 ? 3 : 1;
+
 template <typename T, int VPL, int TPR>
-__global__ __launch_bounds__(256) void norm_backward_kernel(br_norm_shape s, int tile, const T* __restrict__ dout, const float* __restrict__ x, const float* __restrict__ mean,
+__global__ __launch_bounds__(256, (NORM_PER_CU<VPL, TPR>)) void norm_backward_kernel(br_norm_shape s, int tile, const T* __restrict__ dout, const float* __restrict__ x, const float* __restrict__ mean,
                                                             const float* __restrict__ rstd, const float* __restrict__ mods, const float* residual, float* dx,
                                                             float* __restrict__ part, int* __restrict__ tile_group) {
   __shared__ float red[16];
@@ -204,20 +208,20 @@ __global__ __launch_bounds__(256) void norm_backward_kernel(br_norm_shape s, int
   }
 }
 
-// dmods of group blockIdx.y, 64 of the 2 H columns: 16 slices of the tiles, joined in their order.
-__global__ __launch_bounds__(256) void norm_columns_kernel(br_norm_shape s, int n_tiles, const float* __restrict__ part, const int* __restrict__ tile_group, float* __restrict__ dmods) {
-  __shared__ float4 sums[256];
+// dmods of group blockIdx.y, 64 of the 2 H columns: 64 slices of the tiles, joined in their order.
+__global__ __launch_bounds__(1024) void norm_columns_kernel(br_norm_shape s, int n_tiles, const float* __restrict__ part, const int* __restrict__ tile_group, float* __restrict__ dmods) {
+  __shared__ float4 sums[1024];
   const int H = s.hidden, group = blockIdx.y, c = (blockIdx.x * 16 + (threadIdx.x & 15)) * 4, slice = threadIdx.x >> 4;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
   if (c < 2 * H) {
     constexpr int U = 8;
-    for (int t0 = slice; t0 < n_tiles; t0 += 16 * U) {
+    for (int t0 = slice; t0 < n_tiles; t0 += 64 * U) {
       float4 v[U];
       bool in[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) in[u] = t0 + 16 * u < n_tiles && tile_group[min(t0 + 16 * u, n_tiles - 1)] == group;
+      for (int u = 0; u < U; ++u) in[u] = t0 + 64 * u < n_tiles && tile_group[min(t0 + 64 * u, n_tiles - 1)] == group;
 #pragma unroll
-      for (int u = 0; u < U; ++u) v[u] = in[u] ? load4(part + (size_t)(t0 + 16 * u) * 2 * H + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int u = 0; u < U; ++u) v[u] = in[u] ? load4(part + (size_t)(t0 + 64 * u) * 2 * H + c) : make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         acc.x += v[u].x;
@@ -227,26 +231,25 @@ __global__ __launch_bounds__(256) void norm_columns_kernel(br_norm_shape s, int 
       }
     }
   }
+  auto add = [](float4& x, const float4& y) {
+    x.x += y.x;
+    x.y += y.y;
+    x.z += y.z;
+    x.w += y.w;
+  };
   sums[threadIdx.x] = acc;
   __syncthreads();
+  if (slice < 8) {
+#pragma unroll
+    for (int k = 1; k < 8; ++k) add(acc, sums[threadIdx.x + k * 128]);
+    sums[threadIdx.x] = acc;
+  }
+  __syncthreads();
   if (slice == 0 && c < 2 * H) {
-    for (int k = 1; k < 16; ++k) {
-      const float4 o = sums[k * 16 + threadIdx.x];
-      acc.x += o.x;
-      acc.y += o.y;
-      acc.z += o.z;
-      acc.w += o.w;
-    }
+#pragma unroll
+    for (int k = 1; k < 8; ++k) add(acc, sums[threadIdx.x + k * 16]);
     store4(dmods + (size_t)group * s.mods_stride + (c < H ? s.shift_off + c : s.scale_off + c - H), acc.x, acc.y, acc.z, acc.w);
   }
-}
-
-// Rows of a tile of the backward pass: three workgroups a compute unit, four rows at least.
-static int norm_tile(const br_norm_shape& s) { return std::max(4, cdiv(s.rows, 3LL * device_cu_count())); }
-
-size_t norm_train_workspace(const br_norm_shape& s) {
-  const long long tiles = doc_tiles_most(s.n_docs, s.rows, norm_tile(s));
-  return align_up((size_t)tiles * 2 * s.hidden * 4, 256) + (size_t)tiles * 4;
 }
 
 // f(columns a thread in pieces of four, threads a row)
@@ -268,6 +271,18 @@ static void norm_form(int H, F f) {
   else if (g <= 8) with(BR_V(8), G{});
   else with(BR_V(16), G{});
 #undef BR_V
+}
+
+// Rows of a tile of the backward pass: as many workgroups as the units hold at once, four rows at least.
+static int norm_tile(const br_norm_shape& s) {
+  int per_cu = 1;
+  norm_form(s.hidden, [&](auto Vc, auto Tc) { per_cu = NORM_PER_CU<decltype(Vc)::value, decltype(Tc)::value>; });
+  return std::max(4, cdiv(s.rows, (long long)per_cu * device_cu_count()));
+}
+
+size_t norm_train_workspace(const br_norm_shape& s) {
+  const long long tiles = doc_tiles_most(s.n_docs, s.rows, norm_tile(s));
+  return align_up((size_t)tiles * 2 * s.hidden * 4, 256) + (size_t)tiles * 4;
 }
 
 br_status launch_norm_forward(const br_norm_shape& s, const float* x, const float* mods, void* out, float* mean, float* rstd, hipStream_t st) {
@@ -294,7 +309,7 @@ br_status launch_norm_backward(const br_norm_shape& s, const void* dout, const f
     else hipLaunchKernelGGL((norm_backward_kernel<float, VPL, TPR>), dim3(tiles), dim3(256), 0, st, s, tile, (const float*)dout, x, mean, rstd, mods, residual, dx, part, tile_group);
   });
   BR_LAUNCH_CHECK();
-  hipLaunchKernelGGL(norm_columns_kernel, dim3(cdiv(2LL * s.hidden, 64), s.n_groups), dim3(256), 0, st, s, tiles, part, tile_group, dmods);
+  hipLaunchKernelGGL(norm_columns_kernel, dim3(cdiv(2LL * s.hidden, 64), s.n_groups), dim3(1024), 0, st, s, tiles, part, tile_group, dmods);
   BR_LAUNCH_CHECK();
   return BR_OK;
 }
