@@ -2,7 +2,7 @@
 //   mu_r = a_z z_parent + a_v v_r,  logp_e = c0 - h |z_e - mu_r|^2,  rho_e = exp(logp_e - logp_old_e)
 //   d(-J)/dv_r = sum_e w_e (z_e - mu_r),  w_e = -rho_e A_e / n * 2 h a_v, 0 where the clipped term is the smaller one
 // Two launches: squares of the differences by slices of a latent, then, once every slice is known, the gradient.  The second reads again what the
-// first read; up to 256 MB of it comes out of the memory-side cache.
+// first read, for edges that are not clipped; up to 256 MB of it comes out of the memory-side cache.
 #include "dit.h"
 #include "train.h"
 
@@ -40,6 +40,27 @@ __device__ inline float4 obj_mean(const ObjRow& o, long long at) {
   return make_float4(fmaf(o.a_z, a.x, o.a_v * b.x), fmaf(o.a_z, a.y, o.a_v * b.y), fmaf(o.a_z, a.z, o.a_v * b.z), fmaf(o.a_z, a.w, o.a_v * b.w));
 }
 
+__device__ inline float obj_square(const float4& x, const float4& m) {
+  const float a = x.x - m.x, b = x.y - m.y, c = x.z - m.z, d = x.w - m.w;
+  return fmaf(a, a, b * b) + fmaf(c, c, d * d);
+}
+__device__ inline void add_weighted(float4& g, float w, const float4& x, const float4& m) {
+  g.x = fmaf(w, x.x - m.x, g.x);
+  g.y = fmaf(w, x.y - m.y, g.y);
+  g.z = fmaf(w, x.z - m.z, g.z);
+  g.w = fmaf(w, x.w - m.w, g.w);
+}
+// The row that holds edge e: row_first[row] <= e < row_first[row + 1].
+__device__ inline int obj_row_of(const br_edge_set& s, int e) {
+  int lo = 0, hi = s.n_rows;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (s.row_first[mid] <= e) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
 // part[e * slices + slice] = sum over the slice of (z_e - mu)^2
 template <int Q>
 __global__ __launch_bounds__(OBJ_THREADS) void objective_squares_kernel(br_edge_set s, int slices, const float* __restrict__ z, const float* __restrict__ v, double* __restrict__ part) {
@@ -63,10 +84,7 @@ __global__ __launch_bounds__(OBJ_THREADS) void objective_squares_kernel(br_edge_
     }
     float acc = 0.f;
 #pragma unroll
-    for (int q = 0; q < Q; ++q) {
-      const float a = x[q].x - m[q].x, b = x[q].y - m[q].y, cc = x[q].z - m[q].z, d = x[q].w - m[q].w;
-      acc += fmaf(a, a, b * b) + fmaf(cc, cc, d * d);
-    }
+    for (int q = 0; q < Q; ++q) acc += obj_square(x[q], m[q]);
     const double w = wave_sum_d((double)acc);
     __syncthreads();
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = w;
@@ -90,6 +108,8 @@ __device__ inline ObjTerm obj_term(const br_edge_set& s, double squares, double 
   return t;
 }
 
+__device__ inline float obj_weight(const ObjTerm& t, const ObjRow& o) { return (float)(t.weight * 2.0 * o.h * (double)o.a_v); }
+
 // Workgroup 0: J and the log-densities, an edge a thread.  The others: a slice of a row's gradient.
 template <int Q>
 __global__ __launch_bounds__(OBJ_THREADS) void objective_grad_kernel(br_edge_set s, int slices, double inv_n, const float* __restrict__ z, const float* __restrict__ v,
@@ -99,12 +119,7 @@ __global__ __launch_bounds__(OBJ_THREADS) void objective_grad_kernel(br_edge_set
     __shared__ double red[4];
     double sum = 0.0;
     for (int e = threadIdx.x; e < s.n_edges; e += OBJ_THREADS) {
-      int lo = 0, hi = s.n_rows;  // the row that holds e: row_first[lo] <= e < row_first[hi]
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (s.row_first[mid] <= e) lo = mid;
-        else hi = mid;
-      }
+      const int lo = obj_row_of(s, e);
       double sq = 0.0;
 #pragma unroll 8
       for (int i = 0; i < slices; ++i) sq += part[(size_t)e * slices + i];
@@ -125,34 +140,78 @@ __global__ __launch_bounds__(OBJ_THREADS) void objective_grad_kernel(br_edge_set
   const long long base = (long long)slice * (OBJ_THREADS * 4 * Q) + threadIdx.x * 4;
   float4 m[Q], g[Q];
 #pragma unroll
-  for (int q = 0; q < Q; ++q) {
-    const long long at = base + q * (OBJ_THREADS * 4);
-    m[q] = at < s.D ? obj_mean(o, at) : make_float4(0.f, 0.f, 0.f, 0.f);
-    g[q] = make_float4(0.f, 0.f, 0.f, 0.f);
-  }
+  for (int q = 0; q < Q; ++q) m[q] = g[q] = make_float4(0.f, 0.f, 0.f, 0.f);
+  bool have = false;  // the mean: read for the first edge that counts (a row whose edges are all clipped reads nothing)
   for (int e = o.e0; e < o.e1; ++e) {
     double sq = 0.0;
     for (int i = 0; i < slices; ++i) sq += part[(size_t)e * slices + i];  // (the same order as above: the same rho)
     const int node = in_range(s.edge_ids[e], s.n_nodes);
     const ObjTerm t = obj_term(s, sq, o.h, o.c0, logp_old[node], adv[node], inv_n);
     if (t.weight == 0.0) continue;
-    const float w = (float)(t.weight * 2.0 * o.h * (double)o.a_v);
+    const float w = obj_weight(t, o);
     const float* c = z + (size_t)node * s.D;
+    float4 x[Q];
 #pragma unroll
     for (int q = 0; q < Q; ++q) {
       const long long at = base + q * (OBJ_THREADS * 4);
-      if (at >= s.D) continue;
-      const float4 x = *reinterpret_cast<const float4*>(c + at);
-      g[q].x = fmaf(w, x.x - m[q].x, g[q].x);
-      g[q].y = fmaf(w, x.y - m[q].y, g[q].y);
-      g[q].z = fmaf(w, x.z - m[q].z, g[q].z);
-      g[q].w = fmaf(w, x.w - m[q].w, g[q].w);
+      x[q] = at < s.D ? *reinterpret_cast<const float4*>(c + at) : make_float4(0.f, 0.f, 0.f, 0.f);
+      if (!have && at < s.D) m[q] = obj_mean(o, at);
     }
+    have = true;
+#pragma unroll
+    for (int q = 0; q < Q; ++q) add_weighted(g[q], w, x[q], m[q]);
   }
 #pragma unroll
   for (int q = 0; q < Q; ++q) {
     const long long at = base + q * (OBJ_THREADS * 4);
     if (at < s.D) *reinterpret_cast<float4*>(grad + (size_t)r * s.D + at) = g[q];
+  }
+}
+
+// Small sets in one launch of one workgroup, an edge, then a row, a wavefront at a time: the two launches above are 3 us each and 3 us of the host's.
+constexpr int OBJ_SMALL_EDGES = 512;
+constexpr long long OBJ_SMALL_VALUES = 1 << 15;
+__global__ __launch_bounds__(1024) void objective_small_kernel(br_edge_set s, double inv_n, const float* __restrict__ z, const float* __restrict__ v,
+                                                               const float* __restrict__ logp_old, const float* __restrict__ adv, float* __restrict__ J, float* __restrict__ logp_new,
+                                                               float* __restrict__ grad, unsigned char* __restrict__ clipped) {
+  __shared__ double squares[OBJ_SMALL_EDGES], red[16];
+  __shared__ float weight[OBJ_SMALL_EDGES];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  for (int e = wave; e < s.n_edges; e += 16) {
+    const ObjRow o = obj_row(s, z, v, obj_row_of(s, e));
+    const float* c = z + (size_t)in_range(s.edge_ids[e], s.n_nodes) * s.D;
+    double acc = 0.0;
+    for (long long at = lane * 4; at < s.D; at += 256) acc += obj_square(*reinterpret_cast<const float4*>(c + at), obj_mean(o, at));
+    acc = wave_sum_d(acc);
+    if (lane == 0) squares[e] = acc;
+  }
+  __syncthreads();
+  double sum = 0.0;
+  for (int e = threadIdx.x; e < s.n_edges; e += 1024) {
+    const ObjRow o = obj_row(s, z, v, obj_row_of(s, e));
+    const int node = in_range(s.edge_ids[e], s.n_nodes);
+    const ObjTerm t = obj_term(s, squares[e], o.h, o.c0, logp_old[node], adv[node], inv_n);
+    sum += t.term;
+    weight[e] = obj_weight(t, o);
+    logp_new[e] = (float)t.logp;
+    if (clipped) clipped[e] = t.clipped;
+  }
+  sum = wave_sum_d(sum);
+  if (lane == 0) red[wave] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int k = 1; k < 16; ++k) sum += red[k];
+    J[0] = (float)sum;
+  }
+  for (int r = wave; r < s.n_rows; r += 16) {
+    const ObjRow o = obj_row(s, z, v, r);
+    for (long long at = lane * 4; at < s.D; at += 256) {
+      const float4 m = obj_mean(o, at);
+      float4 g = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int e = o.e0; e < o.e1; ++e)
+        if (weight[e] != 0.f) add_weighted(g, weight[e], *reinterpret_cast<const float4*>(z + (size_t)in_range(s.edge_ids[e], s.n_nodes) * s.D + at), m);
+      *reinterpret_cast<float4*>(grad + (size_t)r * s.D + at) = g;
+    }
   }
 }
 
@@ -169,6 +228,11 @@ br_status launch_objective_grad(const br_edge_set& e, const float* z, const floa
   BR_REQUIRE(n < 0x7FFFFFFFLL, BR_ESHAPE, "br_grpo_backward: too many rows for one launch");
   const double inv_n = 1.0 / (double)(e.n_total > 0 ? e.n_total : e.n_edges);
   double* part = reinterpret_cast<double*>(ws);
+  if (e.n_edges <= OBJ_SMALL_EDGES && (long long)e.n_edges * e.D <= OBJ_SMALL_VALUES) {
+    hipLaunchKernelGGL(objective_small_kernel, dim3(1), dim3(1024), 0, st, e, inv_n, z, v, logp_old, adv, J, logp_new, grad, clipped);
+    BR_LAUNCH_CHECK();
+    return BR_OK;
+  }
   auto run = [&](auto Qc) {
     constexpr int Q = decltype(Qc)::value;
     hipLaunchKernelGGL(objective_squares_kernel<Q>, dim3((unsigned)n), dim3(OBJ_THREADS), 0, st, e, slices, z, v, part);
