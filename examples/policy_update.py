@@ -1,0 +1,185 @@
+"""A policy iteration with its update: rollout, rewards, advantages and pruning by the library as ever, then optimizer steps on the velocity network
+with the library's training operators -- packed attention and modulated LayerNorm inside an autograd graph, the gradient of the clipped objective at
+its end, AdamW over all tensors.  The optimizer writes the very tensors that the library's model reads, so the next rollout is the updated policy's.
+
+    python examples/policy_update.py [--net small] [--updates 4] [--state-bits 8]
+"""
+import argparse
+import os
+import sys
+
+import torch
+import torch.nn.functional as F
+
+sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+from paper_2509_06040_amd import binding as br  # noqa: E402
+from paper_2509_06040_amd import synth  # noqa: E402
+
+NETS = {
+    "tiny": synth.WORKLOADS["tiny"]["model"],                                                            # fp32
+    "small": synth.model_cfg(2, 128, 2, (16, 1, 16, 16), (1, 2, 2), 13, synth.BF16),                      # two heads of 64
+}
+
+
+class Attention(torch.autograd.Function):
+    """Documents packed along the tokens; qkv [tokens, 3, heads, head_dim]."""
+
+    @staticmethod
+    def forward(ctx, qkv, off):
+        q, k, v = qkv.unbind(1)
+        out, lse = torch.empty(q.shape, dtype=q.dtype, device=q.device), torch.empty(q.shape[1], q.shape[0], device=q.device)
+        room = br.attention_workspace_bytes(q, k, v, off, off, False)
+        br.attention_forward(q, k, v, off, off, out, lse, torch.empty(room, dtype=torch.uint8, device=q.device) if room else None)
+        ctx.save_for_backward(qkv, off, out, lse)
+        return out
+
+    @staticmethod
+    def backward(ctx, dout):
+        qkv, off, out, lse = ctx.saved_tensors
+        (q, k, v), dqkv = qkv.unbind(1), torch.empty_like(qkv)
+        work = torch.empty(br.attention_workspace_bytes(q, k, v, off, off, True), dtype=torch.uint8, device=q.device)
+        br.attention_backward(dout.contiguous(), q, k, v, out, lse, off, off, *dqkv.unbind(1), work)
+        return dqkv, None
+
+
+class Norm(torch.autograd.Function):
+    """LN(x)(1 + scale) + shift with the vectors `shift` and `scale` (their numbers) of mods [groups, vectors, hidden].  Also gives x on, so that the
+    gradient of the stream past the norm joins in the same pass."""
+
+    @staticmethod
+    def forward(ctx, x, mods, shift, scale, off, group, dtype):
+        H, out = x.shape[1], torch.empty(x.shape, dtype=dtype, device=x.device)
+        mean, rstd = torch.empty(x.shape[0], device=x.device), torch.empty(x.shape[0], device=x.device)
+        mods = mods.contiguous()
+        br.layer_norm_forward(x, mods.flatten(1), shift * H, scale * H, off, group, out, mean, rstd)
+        ctx.save_for_backward(x, mods, mean, rstd, off, group)
+        ctx.at = (shift * H, scale * H)
+        return out, x.view_as(x)
+
+    @staticmethod
+    def backward(ctx, dout, dx):
+        x, mods, mean, rstd, off, group = ctx.saved_tensors
+        rows = mods.flatten(1)
+        dmods, dout, out = torch.zeros_like(rows), dout.contiguous(), torch.empty_like(x)
+        work = torch.empty(br.layer_norm_workspace_bytes(x, dout, rows, *ctx.at, off, group), dtype=torch.uint8, device=x.device)
+        br.layer_norm_backward(dout, x, mean, rstd, rows, *ctx.at, off, group, dx.contiguous(), out, dmods, work)
+        return out, dmods.view_as(mods), None, None, None, None, None
+
+
+class Policy:
+    """The velocity network with its parameters: fp32 masters, the tensors that the library's model reads (bf16 copies of the matrices in a bf16 network, else
+    the masters themselves) and the optimizer over them."""
+
+    def __init__(self, cfg, seed=0, state_bits=32, lr=1e-4, device="cuda"):
+        self.cfg, self.sizes, self.T = cfg, synth.model_sizes(cfg), torch.bfloat16 if cfg["dtype"] == synth.BF16 else torch.float32
+        self.W = br.upload_weights(cfg, synth.make_weights(cfg, seed), device)
+        self.model = br.Model(cfg, self.W)
+        self.names = [n for n in br.WEIGHT_ORDER if n != "pos"]
+        for n in self.names:
+            self.W[n].requires_grad_()
+            self.W[n].grad = torch.zeros_like(self.W[n])
+        self.optimizers = []
+        for dtype in sorted({self.W[n].dtype for n in self.names}, key=str):  # (gradients of a handle are of one type)
+            w = [self.W[n].detach() for n in self.names if self.W[n].dtype == dtype]
+            g = [self.W[n].grad for n in self.names if self.W[n].dtype == dtype]
+            matrix = [n.endswith("_w") for n in self.names if self.W[n].dtype == dtype]
+            kw = {}
+            if dtype == torch.bfloat16:
+                kw["copies"], w = w, [x.float() for x in w]
+            if state_bits == 8:
+                m, v = ([torch.zeros(x.numel(), dtype=torch.uint8, device=device) for x in w] for _ in range(2))
+                kw["m_scales"], kw["v_scales"] = ([torch.zeros((x.numel() + 255) // 256, device=device) for x in w] for _ in range(2))
+            else:
+                m, v = ([torch.zeros_like(x) for x in w] for _ in range(2))
+            self.optimizers.append(br.AdamW(w, g, m, v, weight_decay=[0.01 if x else 0.0 for x in matrix], lr=lr, seed=seed, **kw))
+
+    def velocity(self, z, t, cond):
+        """z [B, D] fp32, t [B], cond [B, tokens, cond_dim] -> [B, D], with its graph."""
+        c, W, T, B = self.cfg, self.W, self.T, z.shape[0]
+        H, NH, n, L = c["hidden"], c["n_heads"], self.sizes["n_img"], self.sizes["L"]
+        linear = lambda x, name, k=None: F.linear(x.to(T), W[name + "_w"] if k is None else W[name + "_w"][k]).float() + (W[name + "_b"] if k is None else W[name + "_b"][k])  # noqa: E731
+        freq = torch.exp(-torch.arange(128, device=z.device, dtype=torch.float64) * (torch.log(torch.tensor(10000.0, dtype=torch.float64)) / 128))
+        a = 1000.0 * t.double()[:, None] * freq
+        ct = linear(F.silu(linear(torch.cat([a.cos(), a.sin()], 1).float(), "t1")), "t2")
+        cvec = ct + linear(cond.float().mean(1), "pool")
+        mods = linear(F.silu(cvec), "ada")
+        g, p = (c["latent_t"] // c["patch_t"], c["latent_h"] // c["patch_h"], c["latent_w"] // c["patch_w"]), (c["patch_t"], c["patch_h"], c["patch_w"])
+        patches = z.view(B, c["latent_c"], g[0], p[0], g[1], p[1], g[2], p[2]).permute(0, 2, 4, 6, 1, 3, 5, 7).reshape(B, n, -1)
+        x = torch.cat([linear(patches, "patch") + W["pos"], linear(cond, "cond")], 1).reshape(B * L, H)
+        off, group = torch.arange(B + 1, dtype=torch.int32, device=z.device) * L, torch.arange(B, dtype=torch.int32, device=z.device)
+        for k in range(c["n_blocks"]):
+            m = mods[:, 6 * H * k:6 * H * (k + 1)].reshape(B, 6, H)
+            gate = lambda y, i: (y.view(B, L, H) * m[:, i, None]).view(B * L, H)  # noqa: E731
+            xn, x = Norm.apply(x, m, 0, 1, off, group, T)
+            out = Attention.apply(linear(xn, "qkv", k).to(T).view(B * L, 3, NH, H // NH), off)
+            x = x + gate(linear(out.reshape(B * L, H), "proj", k), 2)
+            xn, x = Norm.apply(x, m, 3, 4, off, group, T)
+            x = x + gate(linear(F.gelu(linear(xn, "fc1", k), approximate="tanh"), "fc2", k), 5)
+        m = mods[:, 6 * H * c["n_blocks"]:].reshape(B, 2, H)
+        x = x.view(B, L, H)[:, :n].reshape(B * n, H)
+        xn, _ = Norm.apply(x, m, 0, 1, torch.arange(B + 1, dtype=torch.int32, device=z.device) * n, group, T)
+        out = linear(xn, "final").view(B, *g, c["latent_c"], *p)
+        return out.permute(0, 4, 1, 5, 2, 6, 3, 7).reshape(B, -1)
+
+    def step(self):
+        for o in self.optimizers:
+            o.step()
+        for n in self.names:
+            self.W[n].grad.zero_()
+
+
+class Iteration:
+    """One rollout under the policy as it stands, with its rewards, advantages and kept edges."""
+
+    def __init__(self, policy, n_tree=2, T=8, splits=(2, 4, 6), K=2, seed=1, device="cuda"):
+        cfg, D = policy.cfg, policy.sizes["D"]
+        self.tree, self.sched = br.Tree(T, splits, K, n_tree=n_tree), synth.schedule(T, 1.0, logp_mean=True)
+        n, leaves = n_tree * self.tree.n_nodes, n_tree * self.tree.n_leaves
+        self.cond = torch.from_numpy(synth.cond_tokens(cfg, n_tree)).to(device).to(policy.T)
+        self.z, self.logp_old = torch.empty(n, D, device=device), torch.empty(n, device=device)
+        self.work = torch.empty(br.workspace_bytes(self.tree, policy.model, leaves), dtype=torch.uint8, device=device)
+        br.rollout(self.tree, policy.model, self.sched, seed, list(range(n_tree)), self.cond, self.z, self.logp_old, None, self.work)
+        latent, rewards = (cfg["latent_c"], cfg["latent_t"], cfg["latent_h"], cfg["latent_w"]), torch.empty(leaves, device=device)
+        room = torch.empty(max(256, br.reward_scratch_bytes(self.tree, br.REWARD_LINEAR, latent)), dtype=torch.uint8, device=device)
+        br.leaf_reward(self.tree, self.z, br.REWARD_LINEAR, torch.from_numpy(synth.reward_vector(D, 7)).to(device), 0.0, latent, rewards, room)
+        rbar, self.adv = torch.empty(n, device=device), torch.empty(n, device=device)
+        br.fuse_advantage(self.tree, rewards, self.logp_old, 1.0, 1e-8, 0, synth.ADV_CLIP, rbar, self.adv)
+        kept, count = torch.empty(n_tree * self.tree.n_edges, dtype=torch.int32, device=device), torch.zeros(1, dtype=torch.int32, device=device)
+        br.prune(self.tree, rewards, br.PRUNE_EXTREME, 2, None, kept, count)
+        self.ids = kept[:int(count)].contiguous()
+        self.host_ids = self.ids.cpu().numpy()
+        parent, first, coef = br.edge_rows(self.tree, self.sched, D, self.host_ids)
+        put = lambda a: torch.from_numpy(a).to(device)  # noqa: E731
+        self.tables = (self.ids, put(parent), put(first), put(coef))
+        steps = torch.from_numpy(self.tree.depth[parent % self.tree.n_nodes]).long()
+        self.t = torch.from_numpy(self.sched["t"])[steps].to(device)
+        self.of_tree = torch.from_numpy(parent // self.tree.n_nodes).long().to(device)
+        self.J, self.logp_new = torch.empty(1, device=device), torch.empty(len(self.host_ids), device=device)
+
+    def update(self, policy, clip=synth.CLIP_RANGE):
+        """One optimizer step on the kept edges; the objective's value before it (a device tensor)."""
+        v = policy.velocity(self.z[self.tables[1].long()], self.t, self.cond[self.of_tree])
+        grad, w = torch.empty_like(v), v.detach()
+        room = br.grpo_backward_workspace_bytes(self.z, w, *self.tables)
+        br.grpo_backward(self.z, w, *self.tables, self.logp_old, self.adv, clip, self.J, self.logp_new, grad, torch.empty(room, dtype=torch.uint8, device=v.device))
+        v.backward(grad)
+        policy.step()
+        return self.J.clone()
+
+
+def main():
+    a = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
+    a.add_argument("--net", choices=sorted(NETS), default="small")
+    a.add_argument("--iterations", type=int, default=2)
+    a.add_argument("--updates", type=int, default=4)
+    a.add_argument("--state-bits", type=int, choices=(8, 32), default=8)
+    a = a.parse_args()
+    policy = Policy(NETS[a.net], state_bits=a.state_bits)
+    for i in range(a.iterations):
+        it = Iteration(policy, seed=1 + i)
+        values = [float(it.update(policy)) for _ in range(a.updates)]
+        print("iteration %d: %d kept edges, %d rows, J %s" % (i, len(it.host_ids), len(it.t), " -> ".join("%.6f" % x for x in values)), flush=True)
+
+
+if __name__ == "__main__":
+    main()
