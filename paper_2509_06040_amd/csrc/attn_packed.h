@@ -1,6 +1,7 @@
 // What the kernels of attention over packed documents share: arguments, the rows of a workgroup, operands.
 #pragma once
 #include <algorithm>
+#include <cmath>
 
 #include "dit.h"
 #include "docs.h"
@@ -19,13 +20,13 @@ constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 struct AttnArgs {
   br_attn_shape s;
   float scale;
-  int tiles;  // of a head
   const void *q, *k, *v, *out, *dout;
-  float *lse, *ref, *delta;  // ref: lse in powers of two, infinite for a query without keys (its probabilities are zero); delta: dout . out
+  float *lse, *ref, *delta;  // ref: lse in powers of two, infinite for a query without keys (its probabilities are zero); delta: -dout . out
   void *o, *dq, *dk, *dv;
   // Launches of few own rows cut the other side's rows of each document in `parts`, a workgroup each, whose sums (fp32, as they stand) a launch behind joins.
   int parts;
   unsigned blocks;       // workgroups of a part
+  int slots;             // workgroups that the units of a compute die take at once, where the last ones may be cut in halves; else 0
   float *part, *part2;   // [parts][tokens][heads][head_dim]: o, dq or dk; dv
   float *part_ref, *part_sum;  // forward: [parts][heads][tokens]
 };
@@ -58,26 +59,59 @@ __device__ inline T* part_row(T* base, int part, int tokens, int row, int heads,
 
 // Workgroup -> (head, tile of the head).  Workgroups go round-robin over the 8 XCDs: g = gcd(heads, 8) heads are in work at a time, each on 8 / g XCDs, so
 // that the tiles of a document's head find what they share in their XCD's L2.
+//
+// Halves (a.slots > 0): where at most half of a die's slots are left for its last tiles, these are cut in two (16 own rows a wave instead of 32), which take 0.6
+// of a tile's time.
 __host__ __device__ inline int heads_at_a_time(int heads) { return heads % 8 == 0 ? 8 : heads % 4 == 0 ? 4 : heads % 2 == 0 ? 2 : 1; }
-__host__ __device__ inline long long head_tile_blocks(int heads, int tiles) {
-  const int g = heads_at_a_time(heads), each = (tiles + 8 / g - 1) / (8 / g);
-  return (long long)heads / g * each * 8;
+__host__ __device__ inline long long head_tile_blocks(int heads, long long tiles, int slots) {
+  const int g = heads_at_a_time(heads);
+  return (heads / g * ((tiles + 8 / g - 1) / (8 / g)) + slots / 2) * 8;
 }
-__device__ inline bool head_tile(const AttnArgs& a, int heads, int* head, int* tile, int* part) {
-  *part = a.parts == 1 ? 0 : blockIdx.x / a.blocks;
-  const unsigned block = blockIdx.x - *part * a.blocks;  // (a part's workgroups are a multiple of 8)
-  const int tiles = a.tiles, g = heads_at_a_time(heads), dies = 8 / g, each = (tiles + dies - 1) / dies, x = block & 7, t = block >> 3;
-  *head = t / each * g + x % g;
-  *tile = (t - t / each * each) * dies + x / g;
-  return *tile < tiles;
+struct OwnRows {
+  DocSpan span;
+  int row, head, part;
+  bool half;
+};
+__device__ inline bool own_place(const AttnArgs& a, const int* off, int tokens, int heads, int rows, OwnRows* o) {
+  o->part = a.parts == 1 ? 0 : blockIdx.x / a.blocks;
+  const unsigned block = blockIdx.x - o->part * a.blocks;  // (a part's workgroups are a multiple of 8)
+  const int x = block & 7;
+  int second = 0;
+  o->half = false;
+  const bool found = doc_tile_of(off, a.s.n_docs, tokens, rows, [&](int total) {
+    const int g = heads_at_a_time(heads), dies = 8 / g, each = (total + dies - 1) / dies, n = heads / g * each;
+    int t = block >> 3;
+    if (a.slots > 0) {
+      const int whole = n / a.slots * a.slots;
+      if (t >= whole && (n - whole) * 2 <= a.slots) {
+        second = (t - whole) & 1;
+        t = whole + (t - whole) / 2;
+        o->half = true;
+      }
+    }
+    if (t >= n) return -1;
+    const int k = t / each, tile = (t - k * each) * dies + x / g;
+    o->head = k * g + x % g;
+    return tile < total ? tile : -1;
+  }, &o->span, &o->row);
+  if (!found) return false;
+  o->row += second * (rows / 2);
+  return o->row < o->span.end;
 }
 
-// Tiles of `rows` own rows over all heads, in `parts`: sets a.tiles, a.parts, a.blocks; workgroups of the launch.
-inline br_status attn_grid(AttnArgs& a, int tokens, int heads, int rows, int parts, unsigned* blocks) {
+// Tiles of `rows` own rows over all heads, in `parts`, `per_cu` workgroups a unit that may be halved (0: not): sets the fields of a; workgroups of the launch.
+inline br_status attn_grid(AttnArgs& a, int tokens, int heads, int rows, int parts, int per_cu, unsigned* blocks) {
   const long long tiles = doc_tiles_most(a.s.n_docs, tokens, rows);
-  a.tiles = (int)tiles;
   a.parts = parts;
-  const long long n = tiles < 0x7FFFFFFFLL ? head_tile_blocks(heads, a.tiles) : 0x7FFFFFFFLL;
+  // Halves, by the tiles that documents of average length give: where the last round is at most half full, and the first or the second; up to the fourth where a
+  // workgroup has a unit for itself (where two or three share one, those that are left run faster by themselves).  The code of both sizes costs launches that need
+  // one 1 to 2 %.  us without / with: backward, heads of 128, two documents of 4350, 12 heads 766 / 748, six of 1050, 16 heads 251 / 244, two of 525, 8 heads 44 / 32;
+  // of 64, the same 27.6 / 21.5, one of 325, 4 heads 21 / 17; forward, three of 2025, 12 heads of 128 97.4 / 93.5, six of 1050, 16 of 64 48.8 / 45; not: eight of
+  // 2025, 8 heads of 128, 2.04 rounds 142 / 147.
+  const int slots = per_cu * device_cu_count() / 8;
+  const double rounds = (double)heads * ((double)tokens / rows + 0.5 * std::min(a.s.n_docs, tokens)) / 8.0 / std::max(slots, 1);
+  a.slots = parts == 1 && rounds < (per_cu == 1 ? 4.0 : 1.2) && rounds - floor(rounds) <= 0.55 ? slots : 0;
+  const long long n = tiles < 0x7FFFFFFFLL ? head_tile_blocks(heads, tiles, a.slots) : 0x7FFFFFFFLL;
   BR_REQUIRE(n * parts < 0x7FFFFFFFLL, BR_ESHAPE, "attention: too many workgroups for one launch");
   a.blocks = (unsigned)n;
   *blocks = (unsigned)(n * parts);

@@ -129,23 +129,21 @@ constexpr float REF_LIMIT = 2048.f;  // a query's reference moves when eight of 
 // Output and log-sum-exp of 128 queries.  Which reference is subtracted from the scores of a query does not matter, as long as it is the same for all it
 // sums: it is the maximum of some tile, and moves only when a lane's eight probabilities of a tile add up to more than REF_LIMIT, so that no maximum is taken
 // on the way.
-template <int DH>
-__global__ __launch_bounds__(256, (PackForm<DH, Pass::FORWARD>::WPE)) void packed_forward_bf16_kernel(AttnArgs a) {
+template <int DH, int QB>
+static __device__ __forceinline__ void packed_forward_rows(const AttnArgs& a, const OwnRows& place) {
   using F = PackForm<DH, Pass::FORWARD>;
-  constexpr int NB = F::NB, EACH = F::EACH;
   using TP = TilePair<DH>;
-  constexpr int KS = DH / 32, DB = DH / 16, BUF_B = TP::BUF_B, TILE_B = TP::TILE_B, QB = 2;
+  constexpr int NB = F::NB, EACH = F::EACH;
+  constexpr int KS = DH / 32, DB = DH / 16, BUF_B = TP::BUF_B, TILE_B = TP::TILE_B;
   constexpr int NA = 2 * KS, NC = DB, NS = NA + NC, FR = 4, RA = FR - 1;
   static_assert(NS % FR == 0 && NB % 2 == 0 && NB % EACH == 0 && NB >= 2 + 2 * EACH, "");
   char* lds = g_packed_tiles;
-  const int share = a.s.n_heads / a.s.n_kv_heads;
-  int head, tile, part_of, own0;
-  DocSpan own;
-  if (!head_tile(a, a.s.n_heads, &head, &tile, &part_of) || !doc_tile(a.s.q_off, a.s.n_docs, a.s.q_tokens, PACK_OWN, tile, &own, &own0)) return;
+  const int head = place.head, part_of = place.part;
+  const DocSpan own = place.span;
   DocSpan keys = other_rows(a.s.k_off, a.s.n_docs, a.s.k_tokens, own);
   take_part(&keys, a.parts, part_of, PACK_TILE);
-  const int kv = head / share, lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4;
-  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row0 = own0 + wv * 32;
+  const int kv = head / (a.s.n_heads / a.s.n_kv_heads), lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4;
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row0 = place.row + wv * (16 * QB);
   const bool active = row0 < own.end;  // (uniform over the wave)
   const int n_keys = keys.end - keys.first, N = (n_keys + PACK_TILE - 1) / PACK_TILE;
 
@@ -252,7 +250,7 @@ __global__ __launch_bounds__(256, (PackForm<DH, Pass::FORWARD>::WPE)) void packe
         });
       });
       // (each query moves for itself: its result does not depend on which queries share its wave; a score that is not a number makes its own sum one)
-      if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(part[0] <= REF_LIMIT && part[1] <= REF_LIMIT)) != 0, 0)) {
+      if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(part[0] <= REF_LIMIT && part[QB - 1] <= REF_LIMIT)) != 0, 0)) {
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) {
           const bool over = quarters_max(part[qb] <= REF_LIMIT ? 0.f : 1.f) != 0.f;
@@ -320,32 +318,36 @@ __global__ __launch_bounds__(256, (PackForm<DH, Pass::FORWARD>::WPE)) void packe
   }
 }
 
+template <int DH, bool HALVES>
+__global__ __launch_bounds__(256, (PackForm<DH, Pass::FORWARD>::WPE)) void packed_forward_bf16_kernel(AttnArgs a) {
+  OwnRows place;
+  if (!own_place(a, a.s.q_off, a.s.q_tokens, a.s.n_heads, PACK_OWN, &place)) return;
+  if constexpr (HALVES) {
+    if (place.half) return packed_forward_rows<DH, 1>(a, place);
+  }
+  packed_forward_rows<DH, 2>(a, place);
+}
+
 // (dk and dv of head dim 128: 128 accumulators and 64 operands a lane, one wave a SIMD)
-template <int DH, Pass PASS>
-__global__ __launch_bounds__(256, (PackForm<DH, PASS>::WPE)) void packed_grad_bf16_kernel(AttnArgs a) {
+template <int DH, Pass PASS, int QB>
+static __device__ __forceinline__ void packed_grad_rows(const AttnArgs& a, const OwnRows& place) {
   using F = PackForm<DH, PASS>;
+  using TP = TilePair<DH>;
   constexpr bool KEYS = PASS == Pass::KEYS;
   constexpr int NB = F::NB, EACH = F::EACH;
-  using TP = TilePair<DH>;
-  constexpr int KS = DH / 32, DB = DH / 16, BUF_B = TP::BUF_B, TILE_B = TP::TILE_B, QB = 2;
+  constexpr int KS = DH / 32, DB = DH / 16, BUF_B = TP::BUF_B, TILE_B = TP::TILE_B;
   constexpr int NA = 4 * KS, NC = KEYS ? 2 * DB : DB, NS = NA + NC, FR = DH == 128 && KEYS ? 8 : 4, RA = FR - 1;
   constexpr int REFS = NB * BUF_B, REF_B = 2 * PACK_TILE * 4;  // ref and delta of a tile's rows, behind the tiles
   static_assert(NS % FR == 0 && NB % 2 == 0 && NB % EACH == 0 && NB >= 2 + 2 * EACH, "");
   char* lds = g_packed_tiles;
-
-  const int share = a.s.n_heads / a.s.n_kv_heads;
-  int head, tile, part_of, own0;
-  DocSpan own;
-  const int* own_off = KEYS ? a.s.k_off : a.s.q_off;
-  if (!head_tile(a, KEYS ? a.s.n_kv_heads : a.s.n_heads, &head, &tile, &part_of) ||
-      !doc_tile(own_off, a.s.n_docs, KEYS ? a.s.k_tokens : a.s.q_tokens, PACK_OWN, tile, &own, &own0))
-    return;
+  const int share = a.s.n_heads / a.s.n_kv_heads, head = place.head, part_of = place.part;
+  const DocSpan own = place.span;
   DocSpan other = other_rows(KEYS ? a.s.q_off : a.s.k_off, a.s.n_docs, KEYS ? a.s.q_tokens : a.s.k_tokens, own);
   take_part(&other, a.parts, part_of, PACK_TILE);
   const int kv = KEYS ? head : head / share, h0 = KEYS ? head * share : head;
   const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g = lane >> 4;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int row0 = own0 + wv * 32;
+  const int row0 = place.row + wv * (16 * QB);
   const bool active = row0 < own.end;  // (uniform over the wave)
 
   // ---- own rows
@@ -376,7 +378,7 @@ __global__ __launch_bounds__(256, (PackForm<DH, PASS>::WPE)) void packed_grad_bf
       ref[qb] = lse == -INFINITY ? INFINITY : lse * LOG2E;
       if (g == 0 && row0 + qb * 16 + l16 < own.end && part_of == 0) {
         a.ref[at] = ref[qb];
-        a.delta[at] = delta[qb];
+        a.delta[at] = -delta[qb];
       }
     }
   }
@@ -452,12 +454,20 @@ __global__ __launch_bounds__(256, (PackForm<DH, PASS>::WPE)) void packed_grad_bf
       for (int e = 0; e < 8; ++e) pf[1][qb][e] = df[1][qb][e] = (bf16)0.f;  // (tile -1)
     const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
     const float unit = a.scale * LOG2E;
-    f32x4 rv[2], dl[2];  // ref and delta of the tile's rows (KEYS)
+    f32x4 rv[2], dl[2];  // ref and -delta of the tile's rows (KEYS)
+    f32x4 cd[QB];        // -delta of the own queries, four times: what X starts from
+    if constexpr (!KEYS) {
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) {
+        cd[qb] = f32x4{-delta[qb], -delta[qb], -delta[qb], -delta[qb]};
+        asm volatile("" : "+v"(cd[qb]));
+      }
+    }
     auto prob = [&](auto Pc, int e) __attribute__((always_inline)) {
       constexpr int P = decltype(Pc)::value;
       const int b = e / (4 * QB), qb = (e >> 2) % QB, r = e & 3;
       const float p = __builtin_amdgcn_exp2f(fmaf(s[0][b][qb][r], unit, KEYS ? -rv[b][r] : -ref[qb]));
-      const float ds = p * (s[1][b][qb][r] - (KEYS ? dl[b][r] : delta[qb]));
+      const float ds = p * s[1][b][qb][r];
       if constexpr (KEYS) pf[P][qb][b * 4 + r] = (bf16)p;
       df[P][qb][b * 4 + r] = (bf16)ds;
     };
@@ -465,7 +475,7 @@ __global__ __launch_bounds__(256, (PackForm<DH, PASS>::WPE)) void packed_grad_bf
       constexpr int n = decltype(Nc)::value, P = decltype(Pc)::value, qb = decltype(QBc)::value;
       if constexpr (n < NA) {
         constexpr int kind = n & 1, b = n / (2 * KS), ks = (n >> 1) % KS;
-        s[kind][b][qb] = mma(f, kind == 0 ? f1[qb][ks] : f2[qb][ks], ks == 0 ? zero : s[kind][b][qb]);
+        s[kind][b][qb] = mma(f, kind == 0 ? f1[qb][ks] : f2[qb][ks], ks > 0 ? s[kind][b][qb] : kind == 0 ? zero : KEYS ? dl[b] : cd[qb]);
       } else {
         constexpr int i = n - NA, d = KEYS ? i >> 1 : i;
         if constexpr (KEYS && (i & 1) == 0) acc2[d][qb] = mma(f, pf[P][qb], acc2[d][qb]);
@@ -486,6 +496,9 @@ __global__ __launch_bounds__(256, (PackForm<DH, PASS>::WPE)) void packed_grad_bf
       }
       static_for<NS>([&](auto Nc) __attribute__((always_inline)) {
         constexpr int n = decltype(Nc)::value;
+        // (the scores in front: 1 % over both kernels)
+        if constexpr (n == 0) __builtin_amdgcn_s_setprio(1);
+        if constexpr (n == NA) __builtin_amdgcn_s_setprio(0);
         if constexpr (n + RA < NS) fr[(n + RA) % FR] = frag_of(std::integral_constant<int, n + RA>{}, B * BUF_B, BP * BUF_B);
         else fr[(n + RA) % FR] = frag_of(std::integral_constant<int, n + RA - NS>{}, BN * BUF_B, B * BUF_B);
         __builtin_amdgcn_sched_barrier(0);
@@ -566,12 +579,28 @@ __global__ __launch_bounds__(256, (PackForm<DH, PASS>::WPE)) void packed_grad_bf
   }
 }
 
+template <int DH, Pass PASS, bool HALVES>
+__global__ __launch_bounds__(256, (PackForm<DH, PASS>::WPE)) void packed_grad_bf16_kernel(AttnArgs a) {
+  constexpr bool KEYS = PASS == Pass::KEYS;
+  OwnRows place;
+  if (!own_place(a, KEYS ? a.s.k_off : a.s.q_off, KEYS ? a.s.k_tokens : a.s.q_tokens, KEYS ? a.s.n_kv_heads : a.s.n_heads, PACK_OWN, &place)) return;
+  if constexpr (HALVES) {
+    if (place.half) return packed_grad_rows<DH, PASS, 1>(a, place);
+  }
+  packed_grad_rows<DH, PASS, 2>(a, place);
+}
+
 br_status launch_attn_forward_bf16(AttnArgs a, int parts, hipStream_t st) {
   unsigned n;
-  const br_status ok = attn_grid(a, a.s.q_tokens, a.s.n_heads, PACK_OWN, parts, &n);
+  const br_status ok = attn_grid(a, a.s.q_tokens, a.s.n_heads, PACK_OWN, parts, pack_per_cu(a.s.head_dim, 0), &n);
   if (ok != BR_OK) return ok;
-  if (a.s.head_dim == 64) hipLaunchKernelGGL((packed_forward_bf16_kernel<64>), dim3(n), dim3(256), (PackForm<64, Pass::FORWARD>::LDS), st, a);
-  else hipLaunchKernelGGL((packed_forward_bf16_kernel<128>), dim3(n), dim3(256), (PackForm<128, Pass::FORWARD>::LDS), st, a);
+  auto run = [&](auto Dc) {
+    constexpr int DH = decltype(Dc)::value;
+    if (a.slots > 0) hipLaunchKernelGGL((packed_forward_bf16_kernel<DH, true>), dim3(n), dim3(256), (PackForm<DH, Pass::FORWARD>::LDS), st, a);
+    else hipLaunchKernelGGL((packed_forward_bf16_kernel<DH, false>), dim3(n), dim3(256), (PackForm<DH, Pass::FORWARD>::LDS), st, a);
+  };
+  if (a.s.head_dim == 64) run(std::integral_constant<int, 64>{});
+  else run(std::integral_constant<int, 128>{});
   BR_LAUNCH_CHECK();
   return parts > 1 ? launch_attn_join_forward(a, st) : BR_OK;
 }
@@ -580,16 +609,18 @@ template <int DH>
 static br_status grad_launch(AttnArgs a, int parts_q, int parts_k, hipStream_t st) {
   unsigned n;
   if (a.s.q_tokens > 0) {
-    br_status ok = attn_grid(a, a.s.q_tokens, a.s.n_heads, PACK_OWN, parts_q, &n);
+    br_status ok = attn_grid(a, a.s.q_tokens, a.s.n_heads, PACK_OWN, parts_q, pack_per_cu(DH, 1), &n);
     if (ok != BR_OK) return ok;
-    hipLaunchKernelGGL((packed_grad_bf16_kernel<DH, Pass::QUERIES>), dim3(n), dim3(256), (PackForm<DH, Pass::QUERIES>::LDS), st, a);
+    if (a.slots > 0) hipLaunchKernelGGL((packed_grad_bf16_kernel<DH, Pass::QUERIES, true>), dim3(n), dim3(256), (PackForm<DH, Pass::QUERIES>::LDS), st, a);
+    else hipLaunchKernelGGL((packed_grad_bf16_kernel<DH, Pass::QUERIES, false>), dim3(n), dim3(256), (PackForm<DH, Pass::QUERIES>::LDS), st, a);
     BR_LAUNCH_CHECK();
     if (parts_q > 1 && (ok = launch_attn_join_dq(a, st)) != BR_OK) return ok;
   }
   if (a.s.k_tokens > 0) {
-    br_status ok = attn_grid(a, a.s.k_tokens, a.s.n_kv_heads, PACK_OWN, parts_k, &n);
+    br_status ok = attn_grid(a, a.s.k_tokens, a.s.n_kv_heads, PACK_OWN, parts_k, pack_per_cu(DH, 2), &n);
     if (ok != BR_OK) return ok;
-    hipLaunchKernelGGL((packed_grad_bf16_kernel<DH, Pass::KEYS>), dim3(n), dim3(256), (PackForm<DH, Pass::KEYS>::LDS), st, a);
+    if (a.slots > 0) hipLaunchKernelGGL((packed_grad_bf16_kernel<DH, Pass::KEYS, true>), dim3(n), dim3(256), (PackForm<DH, Pass::KEYS>::LDS), st, a);
+    else hipLaunchKernelGGL((packed_grad_bf16_kernel<DH, Pass::KEYS, false>), dim3(n), dim3(256), (PackForm<DH, Pass::KEYS>::LDS), st, a);
     BR_LAUNCH_CHECK();
     if (parts_k > 1 && (ok = launch_attn_join_dkv(a, st)) != BR_OK) return ok;
   }

@@ -145,9 +145,10 @@ __global__ __launch_bounds__(256) void packed_attention_kernel(AttnArgs a) {
   constexpr int KS = K::KS, PS = K::PS, DB = K::DB, NB = K::NB;
   __shared__ __attribute__((aligned(16))) char lds[2 * L::BYTES];
   __shared__ float tops[4][16], sums[4][16];
-  DocSpan span;
-  int first, head, tile, part_of;
-  if (!head_tile(a, a.s.n_heads, &head, &tile, &part_of) || !doc_tile(a.s.q_off, a.s.n_docs, a.s.q_tokens, K::OWN, tile, &span, &first)) return;
+  OwnRows place;
+  if (!own_place(a, a.s.q_off, a.s.q_tokens, a.s.n_heads, K::OWN, &place)) return;
+  const DocSpan span = place.span;
+  const int first = place.row, head = place.head, part_of = place.part;
   DocSpan keys = other_rows(a.s.k_off, a.s.n_docs, a.s.k_tokens, span);
   take_part(&keys, a.parts, part_of, TILE_ROWS);
   const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), kv = head / (a.s.n_heads / a.s.n_kv_heads);
@@ -250,9 +251,10 @@ __global__ __launch_bounds__(256) void packed_attention_dq_kernel(AttnArgs a) {
   using L = Tile<T, DH>;
   constexpr int KS = K::KS, PS = K::PS, DB = K::DB, NB = K::NB;
   __shared__ __attribute__((aligned(16))) char lds[2 * L::BYTES];
-  DocSpan span;
-  int first, head, tile, part_of;
-  if (!head_tile(a, a.s.n_heads, &head, &tile, &part_of) || !doc_tile(a.s.q_off, a.s.n_docs, a.s.q_tokens, K::OWN, tile, &span, &first)) return;
+  OwnRows place;
+  if (!own_place(a, a.s.q_off, a.s.q_tokens, a.s.n_heads, K::OWN, &place)) return;
+  const DocSpan span = place.span;
+  const int first = place.row, head = place.head, part_of = place.part;
   DocSpan keys = other_rows(a.s.k_off, a.s.n_docs, a.s.k_tokens, span);
   take_part(&keys, a.parts, part_of, TILE_ROWS);
   const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), kv = head / (a.s.n_heads / a.s.n_kv_heads);
@@ -279,7 +281,7 @@ __global__ __launch_bounds__(256) void packed_attention_dq_kernel(AttnArgs a) {
       if (lse != -INFINITY) ref = lse * LOG2E;
       if (g == 0 && (WIDE || wave == 0) && part_of == 0) {
         a.ref[at] = ref;
-        a.delta[at] = delta;
+        a.delta[at] = -delta;
       }
     }
   }
@@ -339,10 +341,11 @@ __global__ __launch_bounds__(256) void packed_attention_dkv_kernel(AttnArgs a) {
   using L = Tile<T, DH>;
   constexpr int KS = K::KS, PS = K::PS, DB = K::DB, NB = K::NB;
   __shared__ __attribute__((aligned(16))) char lds[2 * L::BYTES];
-  __shared__ __attribute__((aligned(16))) float refs[2 * TILE_ROWS];  // ref (infinite where there is no query), delta
-  DocSpan span;
-  int first, kv, tile, part_of;
-  if (!head_tile(a, a.s.n_kv_heads, &kv, &tile, &part_of) || !doc_tile(a.s.k_off, a.s.n_docs, a.s.k_tokens, K::OWN, tile, &span, &first)) return;
+  __shared__ __attribute__((aligned(16))) float refs[2 * TILE_ROWS];  // ref (infinite where there is no query), -delta
+  OwnRows place;
+  if (!own_place(a, a.s.k_off, a.s.k_tokens, a.s.n_kv_heads, K::OWN, &place)) return;
+  const DocSpan span = place.span;
+  const int first = place.row, kv = place.head, part_of = place.part;
   DocSpan queries = other_rows(a.s.q_off, a.s.n_docs, a.s.q_tokens, span);
   take_part(&queries, a.parts, part_of, TILE_ROWS);
   const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), share = a.s.n_heads / a.s.n_kv_heads;
@@ -396,7 +399,7 @@ __global__ __launch_bounds__(256) void packed_attention_dkv_kernel(AttnArgs a) {
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         p[b][r] = __builtin_amdgcn_exp2f(fmaf(p[b][r], unit, -ref[r]));
-        ds[b][r] = p[b][r] * (ds[b][r] - delta[r]);
+        ds[b][r] = p[b][r] * (ds[b][r] + delta[r]);
       }
     }
 #pragma unroll
@@ -568,7 +571,7 @@ br_status launch_attn_train_forward(const br_attn_shape& s, const void* q, const
     constexpr int DH = decltype(Dc)::value;
     constexpr bool WIDE = decltype(Wc)::value;
     unsigned n;
-    if ((ok = attn_grid(a, s.q_tokens, s.n_heads, Kernel<T, DH, WIDE>::OWN, plan.forward, &n)) != BR_OK) return;
+    if ((ok = attn_grid(a, s.q_tokens, s.n_heads, Kernel<T, DH, WIDE>::OWN, plan.forward, 0, &n)) != BR_OK) return;
     hipLaunchKernelGGL((packed_attention_kernel<T, DH, WIDE>), dim3(n), dim3(256), 0, st, a);
   });
   if (ok != BR_OK) return ok;
@@ -602,7 +605,7 @@ br_status launch_attn_train_backward(const br_attn_shape& s, const void* dout, c
       constexpr int DH = decltype(Dc)::value;
       constexpr bool WIDE = decltype(Wc)::value;
       unsigned n;
-      if ((ok = attn_grid(a, s.q_tokens, s.n_heads, Kernel<T, DH, WIDE>::OWN, plan.dq, &n)) != BR_OK) return;
+      if ((ok = attn_grid(a, s.q_tokens, s.n_heads, Kernel<T, DH, WIDE>::OWN, plan.dq, 0, &n)) != BR_OK) return;
       hipLaunchKernelGGL((packed_attention_dq_kernel<T, DH, WIDE>), dim3(n), dim3(256), 0, st, a);
     });
     if (ok != BR_OK) return ok;
@@ -615,7 +618,7 @@ br_status launch_attn_train_backward(const br_attn_shape& s, const void* dout, c
       constexpr int DH = decltype(Dc)::value;
       constexpr bool WIDE = decltype(Wc)::value;
       unsigned n;
-      if ((ok = attn_grid(a, s.k_tokens, s.n_kv_heads, Kernel<T, DH, WIDE>::OWN, plan.dkv, &n)) != BR_OK) return;
+      if ((ok = attn_grid(a, s.k_tokens, s.n_kv_heads, Kernel<T, DH, WIDE>::OWN, plan.dkv, 0, &n)) != BR_OK) return;
       hipLaunchKernelGGL((packed_attention_dkv_kernel<T, DH, WIDE>), dim3(n), dim3(256), 0, st, a);
     });
     if (ok != BR_OK) return ok;
