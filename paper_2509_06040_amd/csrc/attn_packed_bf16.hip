@@ -219,16 +219,17 @@ static __device__ __forceinline__ void packed_forward_rows(const AttnArgs& a, co
       part[qb] = b == 0 && r == 0 ? p : part[qb] + p;
       pf[P][qb][b * 4 + r] = (bf16)p;
     };
-    auto step = [&](auto Pc, auto Bc, int j) __attribute__((always_inline)) {
+    auto step = [&](auto Pc, auto Bc, int j, auto LASTc) __attribute__((always_inline)) {  // LASTc: may be the last one
       constexpr int P = decltype(Pc)::value, B = decltype(Bc)::value, BP = (B + NB - 1) % NB, BN = (B + 1) % NB;
       constexpr int NE = 8 * QB;
-      const bool tail = j == N - 1 && n_keys % PACK_TILE != 0;
+      constexpr bool LAST = decltype(LASTc)::value;
+      const bool tail = LAST && j == N - 1 && n_keys % PACK_TILE != 0;
       static_for<NS>([&](auto Nc) __attribute__((always_inline)) {
         constexpr int n = decltype(Nc)::value;
         if constexpr (n + RA < NS) fr[(n + RA) % FR] = frag_of(std::integral_constant<int, n + RA>{}, B * BUF_B, BP * BUF_B);
         else fr[(n + RA) % FR] = frag_of(std::integral_constant<int, n + RA - NS>{}, BN * BUF_B, B * BUF_B);
         __builtin_amdgcn_sched_barrier(0);
-        if constexpr (n == NA) {
+        if constexpr (LAST && n == NA) {
           if (tail) {  // keys past the end
 #pragma unroll
             for (int b = 0; b < 2; ++b)
@@ -268,30 +269,42 @@ static __device__ __forceinline__ void packed_forward_rows(const AttnArgs& a, co
 #pragma unroll
       for (int qb = 0; qb < QB; ++qb) sum[qb] += part[qb];
     };
+    auto behind = [&](auto Bc) __attribute__((always_inline)) {  // the step in buffer B
+      constexpr int B = decltype(Bc)::value;
+      if constexpr (B % EACH == EACH - 1) {
+        tile_turn();
+#pragma unroll
+        for (int i = EACH; i > 0; --i) issue((B + NB - i) % NB);
+      }
+    };
     static_for<RA>([&](auto Nc) __attribute__((always_inline)) { fr[decltype(Nc)::value] = frag_of(Nc, 0, 0); });
     int j = 0;
+    for (; j + NB < N; j += NB)  // (whole rounds of the buffers with more behind them: no questions in between; 2 %.  The backward pass loses 1 to 4 % to that much code)
+      static_for<NB>([&](auto Bc) __attribute__((always_inline)) {
+        constexpr int B = decltype(Bc)::value;
+        step(std::integral_constant<int, B & 1>{}, Bc, 0, std::false_type{});
+        behind(Bc);
+      });
     bool more = true;
     while (more) {
       static_for<NB>([&](auto Bc) __attribute__((always_inline)) {
         if (!more) return;
         constexpr int B = decltype(Bc)::value, P = B & 1;
-        step(std::integral_constant<int, P>{}, Bc, j);
+        step(std::integral_constant<int, P>{}, Bc, j, std::true_type{});
         more = ++j < N;
-        if (more) {
-          if constexpr (B % EACH == EACH - 1) {
-            tile_turn();
-#pragma unroll
-            for (int i = EACH; i > 0; --i) issue((B + NB - i) % NB);
-          }
-        } else {  // values of the last tile
-          static_for<NC>([&](auto Ic) __attribute__((always_inline)) {
-            using Nc = std::integral_constant<int, NA + decltype(Ic)::value>;
-            const bf16x8 f = frag_of(Nc{}, 0, B * BUF_B);
-            static_for<QB>([&](auto Qc) __attribute__((always_inline)) { use(Nc{}, std::integral_constant<int, P>{}, Qc, f); });
-          });
-        }
+        if (more) behind(Bc);
       });
     }
+    auto last = [&](auto Pc, int at) __attribute__((always_inline)) {  // values of the last tile, `at` bytes on
+      static_for<NC>([&](auto Ic) __attribute__((always_inline)) {
+        using Nc = std::integral_constant<int, NA + decltype(Ic)::value>;
+        const bf16x8 f = frag_of(Nc{}, 0, at);
+        static_for<QB>([&](auto Qc) __attribute__((always_inline)) { use(Nc{}, Pc, Qc, f); });
+      });
+    };
+    const int at = (N - 1) % NB * BUF_B;
+    if (N & 1) last(std::integral_constant<int, 0>{}, at);
+    else last(std::integral_constant<int, 1>{}, at);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   }
   if (!active) return;
@@ -518,6 +531,14 @@ static __device__ __forceinline__ void packed_grad_rows(const AttnArgs& a, const
         });
       });
     };
+    auto behind = [&](auto Bc) __attribute__((always_inline)) {  // the step in buffer B
+      constexpr int B = decltype(Bc)::value;
+      if constexpr (B % EACH == EACH - 1) {
+        tile_turn();
+#pragma unroll
+        for (int i = EACH; i > 0; --i) issue((B + NB - i) % NB);
+      }
+    };
     static_for<RA>([&](auto Nc) __attribute__((always_inline)) { fr[decltype(Nc)::value] = frag_of(Nc, 0, 0); });
     int j = 0;
     bool more = true;
@@ -534,21 +555,19 @@ static __device__ __forceinline__ void packed_grad_rows(const AttnArgs& a, const
               if (j * PACK_TILE + (e >> 2) * 16 + 4 * g + (e & 3) >= n_rows) df[P][qb][e] = (bf16)0.f;
         }
         more = ++j < N;
-        if (more) {
-          if constexpr (B % EACH == EACH - 1) {
-            tile_turn();
-#pragma unroll
-            for (int i = EACH; i > 0; --i) issue((B + NB - i) % NB);
-          }
-        } else {  // products of the last tile
-          static_for<NC>([&](auto Ic) __attribute__((always_inline)) {
-            using Nc = std::integral_constant<int, NA + decltype(Ic)::value>;
-            const bf16x8 f = frag_of(Nc{}, 0, B * BUF_B);
-            static_for<QB>([&](auto Qc) __attribute__((always_inline)) { use(Nc{}, std::integral_constant<int, P>{}, Qc, f); });
-          });
-        }
+        if (more) behind(Bc);
       });
     }
+    auto last = [&](auto Pc, int at) __attribute__((always_inline)) {  // products of the last tile, `at` bytes on
+      static_for<NC>([&](auto Ic) __attribute__((always_inline)) {
+        using Nc = std::integral_constant<int, NA + decltype(Ic)::value>;
+        const bf16x8 f = frag_of(Nc{}, 0, at);
+        static_for<QB>([&](auto Qc) __attribute__((always_inline)) { use(Nc{}, Pc, Qc, f); });
+      });
+    };
+    const int at = (N - 1) % NB * BUF_B;
+    if (N & 1) last(std::integral_constant<int, 0>{}, at);
+    else last(std::integral_constant<int, 1>{}, at);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   }
   if (!active) return;
