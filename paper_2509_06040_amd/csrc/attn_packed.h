@@ -148,6 +148,6 @@ br_status launch_attn_join_dq(const AttnArgs& a, hipStream_t st);
 br_status launch_attn_join_dkv(const AttnArgs& a, hipStream_t st);
 // own rows of a workgroup and workgroups a unit of the bf16 kernels: forward, dq, dk and dv
 constexpr int PACK_OWN = 128;
-inline int pack_per_cu(int head_dim, int pass) { return head_dim == 128 ? (pass == 2 ? 1 : 2) : pass == 2 ? 2 : 3; }
+inline int pack_per_cu(int head_dim, int pass) { return head_dim == 128 ? (pass == 2 ? 1 : 2) : pass == 2 ? 2 : pass == 1 ? 3 : 4; }
 
 }  // namespace br

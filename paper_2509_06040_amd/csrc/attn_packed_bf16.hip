@@ -22,8 +22,8 @@ constexpr int PACK_TILE = 32;  // rows of a tile
 enum class Pass { FORWARD, QUERIES, KEYS };
 template <int DH, Pass PASS>
 struct PackForm {
-  static constexpr int WPE = DH == 128 ? (PASS == Pass::KEYS ? 1 : 2) : PASS == Pass::KEYS ? 2 : 3;  // (pack_per_cu)
-  static constexpr int NB = DH == 128 ? (PASS == Pass::KEYS ? 6 : 4) : 6, EACH = NB >= 6 ? 2 : 1;
+  static constexpr int WPE = DH == 128 ? (PASS == Pass::KEYS ? 1 : 2) : PASS == Pass::KEYS ? 2 : PASS == Pass::FORWARD ? 4 : 3;  // (pack_per_cu)
+  static constexpr int NB = DH == 128 ? (PASS == Pass::KEYS ? 6 : 4) : PASS == Pass::FORWARD ? 4 : 6, EACH = NB >= 6 ? 2 : 1;
   static constexpr int LDS = NB * (2 * PACK_TILE * DH * 2 + (PASS == Pass::KEYS ? 2 * PACK_TILE * 4 : 0));
 };
 
