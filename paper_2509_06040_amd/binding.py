@@ -94,11 +94,15 @@ def _h(a, dtype):
     return a, a.ctypes.data_as(C.c_void_p)
 
 
-def _stream():
-    """The current stream of the current device, as its handle (the Stream object that torch.cuda.current_stream makes on the way costs 3 us, a launch 4)."""
+def _stream_handle():
+    """The current stream of the current device, as a number (the Stream object that torch.cuda.current_stream makes on the way costs 3 us, a launch 4)."""
     import torch
     raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    return C.c_void_p(raw(torch.cuda.current_device()) if raw else torch.cuda.current_stream().cuda_stream)
+    return raw(torch.cuda.current_device()) if raw else torch.cuda.current_stream().cuda_stream
+
+
+def _stream():
+    return C.c_void_p(_stream_handle())
 
 
 class Tree:
@@ -368,12 +372,13 @@ def _dtype(x):
     return F32
 
 
-def _token_stride(x):
+def _token_stride(x, tokens, heads, d):
     """Elements between tokens of a [tokens, heads, head_dim] tensor whose heads are adjacent."""
-    tokens, heads, d = x.shape
     t, h, e = x.stride()
-    assert tokens == 0 or (e == 1 and (heads == 1 or h == d)), "heads of a token must be adjacent"
-    return t if tokens > 1 else heads * d
+    if tokens <= 1:
+        t = heads * d
+    assert tokens == 0 or ((e == 1 or d == 1) and (h == d or heads == 1)), "heads of a token must be adjacent"
+    return t
 
 
 def _flat(x, dtype=None):
@@ -385,25 +390,29 @@ def _flat(x, dtype=None):
 
 
 def _room(workspace):
-    return (0, 0) if workspace is None else (_flat(workspace), workspace.numel() * workspace.element_size())
+    return (0, 0) if workspace is None else (_flat(workspace), workspace.nbytes)
 
 
-def _attn_shape(q, k, v, o, q_off, k_off, scale, dq=None, dk=None, dv=None):
+def _attn_shape(q, k, v, o, q_off, k_off, scale, grads=None):
     import torch
-    qs, ks = q.shape, k.shape
-    assert q.dtype is k.dtype is v.dtype is o.dtype and ks == v.shape and qs == o.shape and qs[2] == ks[2], "shapes or types differ"
-    assert q_off.shape == k_off.shape and q_off.dim() == 1, "one offset more than documents"
-    if dq is None:
-        grads = (0, 0, 0)
+    T, i32 = q.dtype, torch.int32
+    tq, nh, d = qs = q.shape
+    tk, nkv, dk = ks = k.shape
+    docs, = q_off.shape
+    assert T is k.dtype is v.dtype is o.dtype and ks == v.shape and qs == o.shape and d == dk, "shapes or types differ"
+    assert k_off.shape == (docs,) and q_off.dtype is k_off.dtype is i32 and q_off.is_contiguous() and k_off.is_contiguous(), "int32 offsets, one more than documents"
+    strides = _token_stride(q, tq, nh, d), _token_stride(k, tk, nkv, d), _token_stride(v, tk, nkv, d), _token_stride(o, tq, nh, d)
+    if grads is None:
+        more = (0, 0, 0)
     else:
-        assert dq.shape == qs and dk.shape == ks and dv.shape == ks and dq.dtype is dk.dtype is dv.dtype is q.dtype, "shapes or types differ"
-        grads = (_token_stride(dq), _token_stride(dk), _token_stride(dv))
-    return _ATTN_SHAPE.pack(_dtype(q), qs[1], ks[1], qs[2], q_off.shape[0] - 1, qs[0], ks[0], 0.0 if scale is None else scale, _token_stride(q), _token_stride(k), _token_stride(v),
-                            _token_stride(o), *grads, _flat(q_off, torch.int32), _flat(k_off, torch.int32))
+        dq, dk, dv = grads
+        assert dq.shape == qs and dk.shape == ks == dv.shape and dq.dtype is dk.dtype is dv.dtype is T, "shapes or types differ"
+        more = _token_stride(dq, tq, nh, d), _token_stride(dk, tk, nkv, d), _token_stride(dv, tk, nkv, d)
+    return _ATTN_SHAPE.pack(_dtype(q), nh, nkv, d, docs - 1, tq, tk, scale or 0.0, *strides, *more, q_off.data_ptr(), k_off.data_ptr())
 
 
 def attention_workspace_bytes(q, k, v, q_off, k_off, backward):
-    return load().br_attention_workspace_bytes(_attn_shape(q, k, v, q, q_off, k_off, None, *((q, k, v) if backward else ())), 1 if backward else 0)
+    return load().br_attention_workspace_bytes(_attn_shape(q, k, v, q, q_off, k_off, None, (q, k, v) if backward else None), 1 if backward else 0)
 
 
 def attention_forward(q, k, v, q_off, k_off, out, lse, workspace=None, scale=None):
@@ -411,17 +420,18 @@ def attention_forward(q, k, v, q_off, k_off, out, lse, workspace=None, scale=Non
     import torch
     s = _attn_shape(q, k, v, out, q_off, k_off, scale)
     assert lse.shape == (q.shape[1], q.shape[0])
-    _check(load().br_attention_forward(s, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _flat(lse, torch.float32), *_room(workspace), _stream()))
+    _check(load().br_attention_forward(s, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _flat(lse, torch.float32), *_room(workspace), _stream_handle()))
 
 
 def attention_backward(dout, q, k, v, out, lse, q_off, k_off, dq, dk, dv, workspace, scale=None):
     """dout laid out as out; dq, dk, dv may be strided (parts of one gradient)."""
     import torch
-    s = _attn_shape(q, k, v, out, q_off, k_off, scale, dq, dk, dv)
-    assert dout.shape == out.shape and dout.dtype is out.dtype and _token_stride(dout) == _token_stride(out), "dout must be laid out as out"
-    assert lse.shape == (q.shape[1], q.shape[0])
+    s = _attn_shape(q, k, v, out, q_off, k_off, scale, (dq, dk, dv))
+    tokens, heads, d = out.shape
+    assert dout.shape == out.shape and dout.dtype is out.dtype and _token_stride(dout, tokens, heads, d) == _token_stride(out, tokens, heads, d), "dout must be laid out as out"
+    assert lse.shape == (heads, tokens)
     _check(load().br_attention_backward(s, dout.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _flat(lse, torch.float32), dq.data_ptr(), dk.data_ptr(),
-                                        dv.data_ptr(), *_room(workspace), _stream()))
+                                        dv.data_ptr(), *_room(workspace), _stream_handle()))
 
 
 def _norm_shape(x, y, mods, shift_off, scale_off, row_off, group):
@@ -440,7 +450,7 @@ def layer_norm_forward(x, mods, shift_off, scale_off, row_off, group, out, mean=
     import torch
     s, f = _norm_shape(x, out, mods, shift_off, scale_off, row_off, group), torch.float32
     assert mean is None or mean.numel() == rstd.numel() == x.shape[0]
-    _check(load().br_layer_norm_forward(s, _flat(x, f), _flat(mods, f), _flat(out), _flat(mean, f), _flat(rstd, f), _stream()))
+    _check(load().br_layer_norm_forward(s, _flat(x, f), _flat(mods, f), _flat(out), _flat(mean, f), _flat(rstd, f), _stream_handle()))
 
 
 def layer_norm_backward(dout, x, mean, rstd, mods, shift_off, scale_off, row_off, group, residual, dx, dmods, workspace):
@@ -449,7 +459,7 @@ def layer_norm_backward(dout, x, mean, rstd, mods, shift_off, scale_off, row_off
     s, f = _norm_shape(x, dout, mods, shift_off, scale_off, row_off, group), torch.float32
     assert dx.shape == x.shape and dmods.shape == mods.shape and mean.numel() == rstd.numel() == x.shape[0] and (residual is None or residual.shape == x.shape)
     _check(load().br_layer_norm_backward(s, _flat(dout), _flat(x, f), _flat(mean, f), _flat(rstd, f), _flat(mods, f), _flat(residual, f), _flat(dx, f), _flat(dmods, f), *_room(workspace),
-                                         _stream()))
+                                         _stream_handle()))
 
 
 def edge_rows(tree, sched, D, edge_ids):
@@ -480,7 +490,7 @@ def grpo_backward(z_nodes, v_rows, edge_ids, row_parent, row_first, row_coef, lo
     s, f = _edge_set(z_nodes, v_rows, edge_ids, row_parent, row_first, row_coef, clip_eps, n_total), torch.float32
     assert grad_v.shape == v_rows.shape and logp_new.shape == edge_ids.shape and logp_old_nodes.numel() == adv_nodes.numel() == z_nodes.shape[0], "shapes differ"
     _check(load().br_grpo_backward(s, _flat(z_nodes, f), _flat(v_rows, f), _flat(logp_old_nodes, f), _flat(adv_nodes, f), _flat(J, f), _flat(logp_new, f), _flat(grad_v, f),
-                                   _flat(clipped), *_room(workspace), _stream()))
+                                   _flat(clipped), *_room(workspace), _stream_handle()))
 
 
 class AdamwTensor(C.Structure):

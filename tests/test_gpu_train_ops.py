@@ -164,6 +164,20 @@ def test_attention_keeps_what_is_not_finite_to_its_own_rows(dtype, d):
     assert np.abs(out[80:] - ref[:, 0]).max() < (0.03 if dtype == "bf16" else 1e-4)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("most", [2, 4, 9, 33])
+def test_attention_gradients_of_short_documents_carry_two_roundings(d, most):
+    """bf16: a correctly rounded value is 2^-8 / sqrt(12) = 0.0011 to 0.0023 of itself off in the mean (0.00166 over evenly spread mantissas).  Gradients of the scores
+    and results are rounded, each once: 0.00166 sqrt(2) = 0.00235; the output's own rounding must not come on top where few keys do not average it out."""
+    r = np.random.default_rng(most)
+    lens = [int(n) for n in r.integers(2, most + 1, 60)]
+    p = Packed("bf16", d, 4, 4, lens, lens, seed=d + most).run()
+    q, k, v, do = (host(t) for t in (p.q, p.k, p.v, p.dout))
+    refs, _ = train.attention_grad(do, q, k, v, p.q_off, p.k_off, p.scale)
+    for t, ref in zip((p.dq, p.dk, p.dv), refs):
+        assert np.linalg.norm(host(t) - ref) < 0.0027 * np.linalg.norm(ref)
+
+
 def test_attention_offsets_out_of_range_stay_inside(lib):
     """Offsets that descend or point past the end: taken as the nearest end, nothing outside the documents' rows is touched."""
     p = Packed("f32", 16, 1, 1, (10, 10), (10, 10))
