@@ -106,6 +106,10 @@ struct TileFrags {
   }
 };
 
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ unsigned two_bf16(float lo, float hi) { return __builtin_bit_cast(unsigned, __builtin_convertvector(f32x2{lo, hi}, bf16x2)); }
+
 __device__ __forceinline__ f32x4 mma(bf16x8 x, bf16x8 y, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, c, 0, 0, 0); }
 
 // Behind every EACH-th step j: the tiles asked for at the last turn have landed, every wave is done with those before tile j, whose buffers take the tiles
@@ -462,12 +466,10 @@ static __device__ __forceinline__ void packed_grad_rows(const AttnArgs& a, const
       else return frags.cols(KEYS ? i >> 1 : i, co + (KEYS ? 1 - (i & 1) : 0) * TILE_B);
     };
     f32x4 s[2][2][QB];               // [S | X][block of 16 rows][own block]
-    bf16x8 pf[2][QB], df[2][QB];     // [parity of the tile][own block]
+    u32x4 pf[2][QB], df[2][QB];      // P and dS, two bf16 values a word [parity of the tile][own block]
     bf16x8 fr[FR];
 #pragma unroll
-    for (int qb = 0; qb < QB; ++qb)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) pf[1][qb][e] = df[1][qb][e] = (bf16)0.f;  // (tile -1)
+    for (int qb = 0; qb < QB; ++qb) pf[1][qb] = df[1][qb] = u32x4{0, 0, 0, 0};  // (tile -1)
     const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
     const float unit = a.scale * LOG2E;
     f32x4 rv[2], dl[2];  // ref and -delta of the tile's rows (KEYS)
@@ -479,13 +481,29 @@ static __device__ __forceinline__ void packed_grad_rows(const AttnArgs& a, const
         asm volatile("" : "+v"(cd[qb]));
       }
     }
-    auto prob = [&](auto Pc, int e) __attribute__((always_inline)) {
-      constexpr int P = decltype(Pc)::value;
-      const int b = e / (4 * QB), qb = (e >> 2) % QB, r = e & 3;
-      const float p = __builtin_amdgcn_exp2f(fmaf(s[0][b][qb][r], unit, KEYS ? -rv[b][r] : -ref[qb]));
-      const float ds = p * s[1][b][qb][r];
-      if constexpr (KEYS) pf[P][qb][b * 4 + r] = (bf16)p;
-      df[P][qb][b * 4 + r] = (bf16)ds;
+    // The probabilities of a tile in 5 operations for each two of a lane's: exponents, exponential, exponential, dS, conversions.
+    constexpr int OPS = 5 * 4 * QB;
+    float p0 = 0.f, p1 = 0.f, ds0 = 0.f, ds1 = 0.f;  // (of the two in work)
+    auto prob = [&](auto Pc, auto Ic) __attribute__((always_inline)) {
+      constexpr int P = decltype(Pc)::value, op = decltype(Ic)::value % 5, two = decltype(Ic)::value / 5, b = two / (2 * QB), qb = (two >> 1) % QB, r = 2 * (two & 1);
+      if constexpr (op == 0) {
+        p0 = fmaf(s[0][b][qb][r], unit, KEYS ? -rv[b][r] : -ref[qb]);
+        p1 = fmaf(s[0][b][qb][r + 1], unit, KEYS ? -rv[b][r + 1] : -ref[qb]);
+        asm volatile("" : "+v"(p0), "+v"(p1));
+      } else if constexpr (op == 1) {
+        p0 = __builtin_amdgcn_exp2f(p0);
+        asm volatile("" : "+v"(p0));
+      } else if constexpr (op == 2) {
+        p1 = __builtin_amdgcn_exp2f(p1);
+        asm volatile("" : "+v"(p1));
+      } else if constexpr (op == 3) {
+        ds0 = p0 * s[1][b][qb][r];
+        ds1 = p1 * s[1][b][qb][r + 1];
+        asm volatile("" : "+v"(ds0), "+v"(ds1));
+      } else {
+        if constexpr (KEYS) pf[P][qb][b * 2 + r / 2] = two_bf16(p0, p1);
+        df[P][qb][b * 2 + r / 2] = two_bf16(ds0, ds1);
+      }
     };
     auto use = [&](auto Nc, auto Pc, auto QBc, const bf16x8& f) __attribute__((always_inline)) {  // Pc: parity of the products' tile
       constexpr int n = decltype(Nc)::value, P = decltype(Pc)::value, qb = decltype(QBc)::value;
@@ -494,15 +512,17 @@ static __device__ __forceinline__ void packed_grad_rows(const AttnArgs& a, const
         s[kind][b][qb] = mma(f, kind == 0 ? f1[qb][ks] : f2[qb][ks], ks > 0 ? s[kind][b][qb] : kind == 0 ? zero : KEYS ? dl[b] : cd[qb]);
       } else {
         constexpr int i = n - NA, d = KEYS ? i >> 1 : i;
-        if constexpr (KEYS && (i & 1) == 0) acc2[d][qb] = mma(f, pf[P][qb], acc2[d][qb]);
-        else acc1[d][qb] = mma(f, df[P][qb], acc1[d][qb]);
+        if constexpr (KEYS && (i & 1) == 0) acc2[d][qb] = mma(f, __builtin_bit_cast(bf16x8, pf[P][qb]), acc2[d][qb]);
+        else acc1[d][qb] = mma(f, __builtin_bit_cast(bf16x8, df[P][qb]), acc1[d][qb]);
       }
     };
     // Step of tile j (parity P, buffer B): its scores, its probabilities behind the first block's, the products of tile j - 1.
     auto step = [&](auto Pc, auto Bc) __attribute__((always_inline)) {
       constexpr int P = decltype(Pc)::value, B = decltype(Bc)::value, BP = (B + NB - 1) % NB, BN = (B + 1) % NB;
-      constexpr int E0 = NA / 2 + 2, EN = NS - 1, NE = 8 * QB;  // the probabilities are taken in these slots
-      constexpr int E1 = NA + 1;                                // those of the second block from here on
+      // Behind each product from G0 on, as many of the operations on the probabilities as spread them evenly: one or two ordinary instructions hide in a product's 16
+      // cycles, eight behind one product and none behind the next three cost a wave 20 cycles.
+      constexpr int G0 = QB * (NA / 2 + 1), GN = QB * NS;
+      static_assert((G0 + GN) / 2 >= QB * NA, "the second block's scores come first");
       if constexpr (KEYS) {
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
@@ -515,24 +535,29 @@ static __device__ __forceinline__ void packed_grad_rows(const AttnArgs& a, const
         // (the scores in front: 1 % over both kernels)
         if constexpr (n == 0) __builtin_amdgcn_s_setprio(1);
         if constexpr (n == NA) __builtin_amdgcn_s_setprio(0);
-        if constexpr (n + RA < NS) fr[(n + RA) % FR] = frag_of(std::integral_constant<int, n + RA>{}, B * BUF_B, BP * BUF_B);
-        else fr[(n + RA) % FR] = frag_of(std::integral_constant<int, n + RA - NS>{}, BN * BUF_B, B * BUF_B);
-        __builtin_amdgcn_sched_barrier(0);
         static_for<QB>([&](auto Qc) __attribute__((always_inline)) {
           use(Nc, std::integral_constant<int, P ^ 1>{}, Qc, fr[n % FR]);
           __builtin_amdgcn_sched_barrier(0);
           if constexpr (decltype(Qc)::value == 0) {
-            if constexpr (n >= E0 && n < E1) {
-#pragma unroll
-              for (int e = NE / 2 * (n - E0) / (E1 - E0); e < NE / 2 * (n - E0 + 1) / (E1 - E0); ++e) prob(Pc, e);
-            } else if constexpr (n >= E1 && n < EN) {
-#pragma unroll
-              for (int e = NE / 2 * (n - E1) / (EN - E1); e < NE / 2 * (n - E1 + 1) / (EN - E1); ++e) prob(Pc, NE / 2 + e);
-            }
+            if constexpr (n + RA < NS) fr[(n + RA) % FR] = frag_of(std::integral_constant<int, n + RA>{}, B * BUF_B, BP * BUF_B);
+            else fr[(n + RA) % FR] = frag_of(std::integral_constant<int, n + RA - NS>{}, BN * BUF_B, B * BUF_B);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+          constexpr int gap = n * QB + decltype(Qc)::value;
+          if constexpr (gap >= G0) {
+            constexpr int from = OPS * (gap - G0) / (GN - G0), to = OPS * (gap - G0 + 1) / (GN - G0);
+            static_for<to - from>([&](auto Ic) __attribute__((always_inline)) { prob(Pc, std::integral_constant<int, from + decltype(Ic)::value>{}); });
             __builtin_amdgcn_sched_barrier(0);
           }
         });
       });
+      // (used in the next step only: left to itself, the compiler moves every second step's exponentials there, where no matrix instruction runs beside them)
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) {
+        u32x4 &x = pf[P][qb], &y = df[P][qb];
+        if constexpr (KEYS) asm volatile("" : "+v"(x));
+        asm volatile("" : "+v"(y));
+      }
     };
     auto behind = [&](auto Bc) __attribute__((always_inline)) {  // the step in buffer B
       constexpr int B = decltype(Bc)::value;
@@ -555,7 +580,7 @@ static __device__ __forceinline__ void packed_grad_rows(const AttnArgs& a, const
           for (int qb = 0; qb < QB; ++qb)
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-              if (j * PACK_TILE + (e >> 2) * 16 + 4 * g + (e & 3) >= n_rows) df[P][qb][e] = (bf16)0.f;
+              if (j * PACK_TILE + (e >> 2) * 16 + 4 * g + (e & 3) >= n_rows) df[P][qb][e >> 1] &= e & 1 ? 0x0000FFFFu : 0xFFFF0000u;
         }
         more = ++j < N;
         if (more) behind(Bc);
@@ -573,7 +598,7 @@ static __device__ __forceinline__ void packed_grad_rows(const AttnArgs& a, const
           }
           d = quarters_sum(d);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) df[0][qb][e] = (bf16)(p[e] * (s[1][e >> 2][qb][e & 3] - d));
+          for (int e = 0; e < 8; e += 2) df[0][qb][e >> 1] = two_bf16(p[e] * (s[1][e >> 2][qb][e & 3] - d), p[e + 1] * (s[1][e >> 2][qb][(e & 3) + 1] - d));
           if (g == 0 && row0 + qb * 16 + l16 < own.end) a.delta[(size_t)head * a.s.q_tokens + row0 + qb * 16 + l16] = -d;
         }
       }
