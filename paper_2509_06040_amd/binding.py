@@ -374,10 +374,12 @@ def _dtype(x):
 
 def _token_stride(x, tokens, heads, d):
     """Elements between tokens of a [tokens, heads, head_dim] tensor whose heads are adjacent."""
+    if x.is_contiguous():
+        return heads * d
     t, h, e = x.stride()
     if tokens <= 1:
         t = heads * d
-    assert tokens == 0 or ((e == 1 or d == 1) and (h == d or heads == 1)), "heads of a token must be adjacent"
+    assert (e == 1 or d == 1) and (h == d or heads == 1), "heads of a token must be adjacent"
     return t
 
 
@@ -393,43 +395,42 @@ def _room(workspace):
     return (0, 0) if workspace is None else (_flat(workspace), workspace.nbytes)
 
 
-def _attn_shape(q, k, v, o, q_off, k_off, scale, grads=None):
+def _attn_shape(q, k, v, o, q_off, k_off, scale, lse=None, dout=None, grads=None):
     import torch
     T, i32 = q.dtype, torch.int32
     tq, nh, d = qs = q.shape
     tk, nkv, dk = ks = k.shape
-    docs, = q_off.shape
+    docs, = offs = q_off.shape
     assert T is k.dtype is v.dtype is o.dtype and ks == v.shape and qs == o.shape and d == dk, "shapes or types differ"
-    assert k_off.shape == (docs,) and q_off.dtype is k_off.dtype is i32 and q_off.is_contiguous() and k_off.is_contiguous(), "int32 offsets, one more than documents"
-    strides = _token_stride(q, tq, nh, d), _token_stride(k, tk, nkv, d), _token_stride(v, tk, nkv, d), _token_stride(o, tq, nh, d)
+    assert k_off.shape == offs and q_off.dtype is k_off.dtype is i32 and q_off.is_contiguous() and k_off.is_contiguous(), "int32 offsets, one more than documents"
+    assert lse is None or lse.shape == (nh, tq), "lse is [heads, tokens]"
+    so = _token_stride(o, tq, nh, d)
     if grads is None:
         more = (0, 0, 0)
     else:
+        assert dout is None or (dout.shape == qs and dout.dtype is T and _token_stride(dout, tq, nh, d) == so), "dout must be laid out as out"
         dq, dk, dv = grads
         assert dq.shape == qs and dk.shape == ks == dv.shape and dq.dtype is dk.dtype is dv.dtype is T, "shapes or types differ"
         more = _token_stride(dq, tq, nh, d), _token_stride(dk, tk, nkv, d), _token_stride(dv, tk, nkv, d)
-    return _ATTN_SHAPE.pack(_dtype(q), nh, nkv, d, docs - 1, tq, tk, scale or 0.0, *strides, *more, q_off.data_ptr(), k_off.data_ptr())
+    return _ATTN_SHAPE.pack(_dtype(q), nh, nkv, d, docs - 1, tq, tk, scale or 0.0, _token_stride(q, tq, nh, d), _token_stride(k, tk, nkv, d), _token_stride(v, tk, nkv, d), so,
+                            *more, q_off.data_ptr(), k_off.data_ptr())
 
 
 def attention_workspace_bytes(q, k, v, q_off, k_off, backward):
-    return load().br_attention_workspace_bytes(_attn_shape(q, k, v, q, q_off, k_off, None, (q, k, v) if backward else None), 1 if backward else 0)
+    return load().br_attention_workspace_bytes(_attn_shape(q, k, v, q, q_off, k_off, None, grads=(q, k, v) if backward else None), 1 if backward else 0)
 
 
 def attention_forward(q, k, v, q_off, k_off, out, lse, workspace=None, scale=None):
     """q, out [tokens, heads, head_dim], k, v [tokens, kv heads, head_dim] (tokens may be strided), offsets int32 [documents + 1], lse [heads, tokens] fp32."""
     import torch
-    s = _attn_shape(q, k, v, out, q_off, k_off, scale)
-    assert lse.shape == (q.shape[1], q.shape[0])
+    s = _attn_shape(q, k, v, out, q_off, k_off, scale, lse)
     _check(load().br_attention_forward(s, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _flat(lse, torch.float32), *_room(workspace), _stream_handle()))
 
 
 def attention_backward(dout, q, k, v, out, lse, q_off, k_off, dq, dk, dv, workspace, scale=None):
     """dout laid out as out; dq, dk, dv may be strided (parts of one gradient)."""
     import torch
-    s = _attn_shape(q, k, v, out, q_off, k_off, scale, (dq, dk, dv))
-    tokens, heads, d = out.shape
-    assert dout.shape == out.shape and dout.dtype is out.dtype and _token_stride(dout, tokens, heads, d) == _token_stride(out, tokens, heads, d), "dout must be laid out as out"
-    assert lse.shape == (heads, tokens)
+    s = _attn_shape(q, k, v, out, q_off, k_off, scale, lse, dout, (dq, dk, dv))
     _check(load().br_attention_backward(s, dout.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _flat(lse, torch.float32), dq.data_ptr(), dk.data_ptr(),
                                         dv.data_ptr(), *_room(workspace), _stream_handle()))
 
