@@ -99,16 +99,14 @@ __device__ inline void quad_codes_store(unsigned char* p, long long at, long lon
 template <int M>
 constexpr float CODE_MOST = (float)(((2 << M) - 1) << 14);
 template <int M>
-__device__ inline float code_value(unsigned code) {  // without a sign
-  const int e = code >> M, f = code & ((1 << M) - 1);
-  return (float)(e > 0 ? (f + (1 << M)) << (e - 1) : f);
+__device__ inline float code_value(unsigned code) {  // without a sign: as e and f stand in fp32, subnormal numbers among them, a power of two below
+  return ldexpf(__builtin_bit_cast(float, code << (23 - M)), 126 + M);
 }
 // The code below y (0 <= y <= CODE_MOST), or the one above it where 16 random bits, as a fraction, reach over.
 template <int M>
 __device__ inline unsigned code_of(float y, unsigned random16) {
   const int e = max((int)(__builtin_bit_cast(unsigned, y) >> 23) - 127 - M, 0);
-  const float q = floorf(ldexpf(y, -e) + (float)random16 * (1.f / 65536.f));
-  return ((unsigned)e << M) + (unsigned)q;
+  return ((unsigned)e << M) + (unsigned)fmaf((float)random16, 1.f / 65536.f, ldexpf(y, -e));  // (the product is exact)
 }
 
 // The largest magnitude of the wavefront's 256 values; as numbers' bits, so that one that is not finite is the largest.
@@ -119,11 +117,19 @@ __device__ inline float wave_top(const float4& v) {
   for (int d = 32; d; d >>= 1) t = max(t, (unsigned)__shfl_xor((int)t, d, 64));
   return __builtin_bit_cast(float, t);
 }
-// Scale of a block and the factor that takes its values to codes.  Blocks without a value above 2^-96 are held as zeros (their scale would leave fp32).
-__device__ inline float block_scale(float top, float most, float* up) {
-  const bool fine = top < INFINITY, some = top > 1.2621774e-29f;
-  *up = fine && some ? most / top : 0.f;
-  return fine ? (some ? top / most : 0.f) : __builtin_nanf("");
+// Scales of a block of m and one of sqrt(v) and the factors that take values to codes, a quarter of the lanes each: one quotient.  Blocks without a value above 2^-96 are held as zeros
+// (their scale would leave fp32).
+struct BlockScales {
+  float m, v, m_up, v_up;
+};
+__device__ inline BlockScales block_scales(float top_m, float top_v) {
+  const int lane = threadIdx.x & 63;
+  const float top = lane & 16 ? top_v : top_m, most = lane & 16 ? CODE_MOST<4> : CODE_MOST<3>;
+  const bool fine = top < INFINITY, some = top > 1.2621774e-29f, up = lane & 32;
+  const float q = (up ? most : top) / (up ? top : most), r = fine ? (some ? q : 0.f) : up ? 0.f : __builtin_nanf("");
+  const int b = __builtin_bit_cast(int, r);
+  auto of = [&](int l) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(b, l)); };
+  return {of(0), of(16), of(32), of(48)};
 }
 
 // What a lane reads of a group: a quad of each tensor, as it lies in memory.
@@ -187,15 +193,14 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamwArgs a) {
       quad_store(reinterpret_cast<float*>(t.v), at, n, wide, q.v);
     } else {
       if (at >= n) q.m = root = make_float4(0.f, 0.f, 0.f, 0.f);  // (with eps = 0 a quotient of zeros; the states of what is not there are 0 as they are)
-      float um, uv;
-      const float sm = block_scale(wave_top(q.m), CODE_MOST<3>, &um), sv = block_scale(wave_top(root), CODE_MOST<4>, &uv);
+      const BlockScales scales = block_scales(wave_top(q.m), wave_top(root));
       uint32_t w[4];
       philox4x32_10(key, (uint32_t)(at >> 2), t.index, a.step, TAG_ADAMW, w);
       unsigned cm = 0, cv = 0;
       auto pack = [&](int i, float mm, float rr) {
-        const unsigned c = code_of<3>(fminf(fabsf(mm) * um, CODE_MOST<3>), w[i] & 0xFFFF) | (mm < 0.f ? 128u : 0u);
+        const unsigned c = code_of<3>(fminf(fabsf(mm) * scales.m_up, CODE_MOST<3>), w[i] & 0xFFFF) | (mm < 0.f ? 128u : 0u);
         cm |= c << (8 * i);
-        cv |= code_of<4>(fminf(rr * uv, CODE_MOST<4>), w[i] >> 16) << (8 * i);
+        cv |= code_of<4>(fminf(rr * scales.v_up, CODE_MOST<4>), w[i] >> 16) << (8 * i);
       };
       pack(0, q.m.x, root.x);
       pack(1, q.m.y, root.y);
@@ -204,8 +209,8 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamwArgs a) {
       quad_codes_store(reinterpret_cast<unsigned char*>(t.m), at, n, wide, cm);
       quad_codes_store(reinterpret_cast<unsigned char*>(t.v), at, n, wide, cv);
       if (lane == 0) {
-        t.m_scale[first / ADAMW_GROUP] = sm;
-        t.v_scale[first / ADAMW_GROUP] = sv;
+        t.m_scale[first / ADAMW_GROUP] = scales.m;
+        t.v_scale[first / ADAMW_GROUP] = scales.v;
       }
     }
     quad_store(t.p, at, n, wide, q.p);

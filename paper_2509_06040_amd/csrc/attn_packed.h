@@ -120,8 +120,9 @@ inline br_status attn_grid(AttnArgs& a, int tokens, int heads, int rows, int par
 
 // Parts of a launch whose own rows make fewer workgroups than the units take at once (`per_cu` each).  They save the time of the steps that others take (step_us for 32
 // rows of an average document, `heads` times over for keys that several heads of queries share) and cost the join: 4 us, and `outputs` fp32 values of every
-// own row's channel written and read by each part (3 TB/s together).  us in one part / as many as this rule gives, heads of 64 in bf16: 20 queries on 1800 keys, 8
-// heads on two over two documents of 750, see the launchers.
+// own row's channel written and read by each part (3 TB/s together).  us in one part / as many as this rule gives: bf16 backward, 8 heads on two, two documents of 750,
+// heads of 64 73 / 38, of 128 116 / 56; 4 heads, one of 1060, 41 / 30 and 64 / 45; four of 1024 queries on 77 keys, heads of 128 47 / 32; fp32 forward, 20 queries on
+// 1800 keys, heads of 128 24 / 15.
 inline int attn_parts(const br_attn_shape& s, long long own_tokens, int own_heads, int own_rows, long long other_tokens, int heads, int per_cu, float step_us, int outputs) {
   if (own_tokens == 0 || other_tokens == 0 || s.n_docs == 0) return 1;
   const long long blocks = std::max<long long>(cdiv(own_tokens, own_rows), std::min<long long>(s.n_docs, own_tokens)) * own_heads;

@@ -5,6 +5,14 @@
 // (X - delta), and the products with the tile's rows, dk += Y1^T dS (dq the same) and dv += Y2^T P.  These wait for the next tile: between its scores' last
 // matrix instructions and theirs stand the exponentials of the tile itself.
 //
+// Both passes take scores anew from q, k and the log-sum-exp: seven products where the formulas have five, nothing of a tile's size in memory and every sum in one
+// wavefront's registers in a fixed order (dq added up over the workgroups of the keys instead would be 85 MB of fp32 for a head of a document of 4600 tokens).
+//
+// Bound by the matrix pipe, the exponentials issued beside it, and the clock that the chip's power leaves (2.0 to 2.3 GHz with random inputs; with inputs of zero
+// 20 to 30 % faster).  Measured: forward, 16 heads of 64, 16 documents of 1025 to 1101 tokens 96 us, 768 TFLOP/s (matrix pipe 32 % busy, VALU 54 %); backward of eight of them 155
+// us, 600 TFLOP/s by the formulas' five products, 840 by the seven; backward, 12 heads of 128, two documents of 4096 to 4608 728 us, 743 and 1041 (matrix pipe 51 % busy for
+// dq, 41 % for dk and dv, VALU 36 and 31 %).  A library product of 8192^3 reaches 1202 on the same card.
+//
 // Tiles come straight from global memory into LDS, rows as they lie, 16-byte chunks permuted per row so that both the fragments of 16 rows
 // and the transposed reads (eight rows, two chunks) spread over the banks.
 #include "attn_packed.h"

@@ -4,6 +4,9 @@
 //
 // A row lies in the registers of TPR threads (a wavefront up to 2048 columns, a workgroup of 256 above), in VPL pieces of four columns a
 // thread.  Statistics are taken in two passes over these registers, as the network's LayerNorm takes them.
+//
+// Every matrix is read or written once.  Measured: forward, 17 000 rows of 1024, bf16 out, 23 us, 4.5 TB/s; backward, 33 000 rows of 1536, fp32 residual and bf16 dout, 156 us,
+// 4.5 TB/s (a copy of 4 GB: 4.75), 6.6 us of them the launch that joins the tiles' column sums.
 #include "dit.h"
 #include "docs.h"
 #include "train.h"
@@ -208,7 +211,7 @@ __global__ __launch_bounds__(256, (NORM_PER_CU<VPL, TPR>)) void norm_backward_ke
   }
 }
 
-// dmods of group blockIdx.y, 64 of the 2 H columns: 64 slices of the tiles, joined in their order.
+// dmods of group blockIdx.y, 64 of the 2 H columns: 64 slices of the tiles, joined in their order.  (6.6 us for 512 tiles of 2 x 1536: the latency of each slice's loads.)
 __global__ __launch_bounds__(1024) void norm_columns_kernel(br_norm_shape s, int n_tiles, const float* __restrict__ part, const int* __restrict__ tile_group, float* __restrict__ dmods) {
   __shared__ float4 sums[1024];
   const int H = s.hidden, group = blockIdx.y, c = (blockIdx.x * 16 + (threadIdx.x & 15)) * 4, slice = threadIdx.x >> 4;

@@ -3,6 +3,8 @@
 //   d(-J)/dv_r = sum_e w_e (z_e - mu_r),  w_e = -rho_e A_e / n * 2 h a_v, 0 where the clipped term is the smaller one
 // Two launches: squares of the differences by slices of a latent, then, once every slice is known, the gradient.  The second reads again what the
 // first read, for edges that are not clipped; up to 256 MB of it comes out of the memory-side cache.
+// Measured: four trees of 16 leaves, latents of 65 536, half of the edges kept: 40 us for the squares (172 MB, 4.3 TB/s), 27 for the gradient (169 MB, 6.2 TB/s).  One launch whose
+// last slice of a row goes on to the gradient: 110 us, its workgroups' round trips follow one another.
 #include "dit.h"
 #include "train.h"
 
