@@ -134,7 +134,7 @@ br_status br_grpo_backward(const br_edge_set* edges, const float* z_nodes, const
  * neighbouring codes at random, with probabilities that keep their mean: a change of 0.1 % a step, which rounding to the
  * nearest would never see, moves a second moment as it should.  The random bits of elements 4 q .. 4 q + 3 of tensor
  * number i are the words of Philox4x32-10 at counter (q, i, step, 4) keyed by `seed`, low halves for m, high ones for sqrt(v).
- * A block with a value that is not finite becomes NaN.
+ * A block with a value that is not finite becomes NaN; one without a value above 2^-96 is held as zeros.
  * ------------------------------------------------------------------------- */
 typedef struct {
   float* param;                        /* dev [n] */

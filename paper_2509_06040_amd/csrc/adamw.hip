@@ -2,8 +2,12 @@
 // no table on the device and can be captured in a graph.  A wavefront takes 256 consecutive elements of a tensor, four a lane: the block of one scale of
 // the states in 8 bits, whose largest value is then a maximum over the wavefront.
 //
-// Loads and stores of whole quads go past the caches, which nothing here is read from twice (240 M parameters, states in 32 bits: plain 1223 us, stores past
-// them 1227, loads too 1151 (5.65 TB/s); in 8 bits 1187, 1185, 1171 with the read-out of their values); the bf16 copies, which the network reads next, stay.
+// 240 M parameters with bf16 gradients and copies: states in 32 bits 1150 us, 5.66 TB/s; in 8 bits 650 to 700 us, 5.4 to 5.8 TB/s, and the read-out of their values 407 us, 5.9.
+// A step in 8 bits has the chip's VALU nearly full (generator, root, quotient, codes): with scales by four quotients, maxima by way of LDS and codes taken apart with integer
+// arithmetic it took 747 to 812.
+//
+// Loads and stores of whole quads go past the caches, which nothing here is read from twice (states in 32 bits: plain 1223 us, stores past
+// them 1227, loads too 1151); the bf16 copies, which the network reads next, stay.
 //
 // Every product, sum, quotient and root is rounded by itself (no contraction): states in 8 bits are the same bits wherever they are computed.
 #include "dit.h"
@@ -109,27 +113,29 @@ __device__ inline unsigned code_of(float y, unsigned random16) {
   return ((unsigned)e << M) + (unsigned)fmaf((float)random16, 1.f / 65536.f, ldexpf(y, -e));  // (the product is exact)
 }
 
-// The largest magnitude of the wavefront's 256 values; as numbers' bits, so that one that is not finite is the largest.
-__device__ inline float wave_top(const float4& v) {
-  auto mag = [](float x) { return __builtin_bit_cast(unsigned, x) & 0x7FFFFFFFu; };
-  unsigned t = max(max(mag(v.x), mag(v.y)), max(mag(v.z), mag(v.w)));
-#pragma unroll
-  for (int d = 32; d; d >>= 1) t = max(t, (unsigned)__shfl_xor((int)t, d, 64));
-  return __builtin_bit_cast(float, t);
-}
-// Scales of a block of m and one of sqrt(v) and the factors that take values to codes, a quarter of the lanes each: one quotient.  Blocks without a value above 2^-96 are held as zeros
-// (their scale would leave fp32).
+// Scales of a block of m and one of sqrt(v) and the factors that take values to codes.  Lower half of the wavefront: m, upper half: sqrt(v); a quarter then each of the four quotients.
+// Magnitudes are compared as numbers' bits, so that one that is not finite is the largest.  Blocks without a value above 2^-96 are held as zeros (their scale would leave fp32).
 struct BlockScales {
   float m, v, m_up, v_up;
 };
-__device__ inline BlockScales block_scales(float top_m, float top_v) {
+__device__ inline BlockScales block_scales(const float4& m, const float4& v) {
+  auto mag = [](float x) { return __builtin_bit_cast(unsigned, x) & 0x7FFFFFFFu; };
+  auto four = [&](const float4& x) { return max(max(mag(x.x), mag(x.y)), max(mag(x.z), mag(x.w))); };
+  auto p = __builtin_amdgcn_permlane32_swap(four(m), four(v), false, false);
+  unsigned t = max((unsigned)p[0], (unsigned)p[1]);
+  p = __builtin_amdgcn_permlane16_swap(t, t, false, false);
+  t = max((unsigned)p[0], (unsigned)p[1]);
+  auto with = [&](auto CTRL) { t = max(t, (unsigned)__builtin_amdgcn_update_dpp(0, (int)t, decltype(CTRL)::value, 0xf, 0xf, true)); };
+  with(std::integral_constant<int, 0x128>{});  // row_ror:8
+  with(std::integral_constant<int, 0x124>{});  // row_ror:4
+  with(std::integral_constant<int, 0x4E>{});   // quad_perm [2,3,0,1]
+  with(std::integral_constant<int, 0xB1>{});   // quad_perm [1,0,3,2]
   const int lane = threadIdx.x & 63;
-  const float top = lane & 16 ? top_v : top_m, most = lane & 16 ? CODE_MOST<4> : CODE_MOST<3>;
-  const bool fine = top < INFINITY, some = top > 1.2621774e-29f, up = lane & 32;
+  const float top = __builtin_bit_cast(float, t), most = lane & 32 ? CODE_MOST<4> : CODE_MOST<3>;
+  const bool fine = top < INFINITY, some = top > 1.2621774e-29f, up = lane & 16;
   const float q = (up ? most : top) / (up ? top : most), r = fine ? (some ? q : 0.f) : up ? 0.f : __builtin_nanf("");
-  const int b = __builtin_bit_cast(int, r);
-  auto of = [&](int l) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(b, l)); };
-  return {of(0), of(16), of(32), of(48)};
+  auto of = [&](int l) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, r), l)); };
+  return {of(0), of(32), of(16), of(48)};
 }
 
 // What a lane reads of a group: a quad of each tensor, as it lies in memory.
@@ -193,7 +199,7 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamwArgs a) {
       quad_store(reinterpret_cast<float*>(t.v), at, n, wide, q.v);
     } else {
       if (at >= n) q.m = root = make_float4(0.f, 0.f, 0.f, 0.f);  // (with eps = 0 a quotient of zeros; the states of what is not there are 0 as they are)
-      const BlockScales scales = block_scales(wave_top(q.m), wave_top(root));
+      const BlockScales scales = block_scales(q.m, root);
       uint32_t w[4];
       philox4x32_10(key, (uint32_t)(at >> 2), t.index, a.step, TAG_ADAMW, w);
       unsigned cm = 0, cv = 0;
