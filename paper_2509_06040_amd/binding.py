@@ -94,11 +94,24 @@ def _h(a, dtype):
     return a, a.ctypes.data_as(C.c_void_p)
 
 
+_f32 = _bf16 = _i32 = _f64 = _raw_stream = _device = None
+
+
+def _torch_names():
+    """What the calls below need of torch, once: a call of small tensors is the host's time, and an import statement and a lookup in it are 0.1 us each."""
+    global _f32, _bf16, _i32, _f64, _raw_stream, _device
+    import torch
+    _f32, _bf16, _i32, _f64 = torch.float32, torch.bfloat16, torch.int32, torch.float64
+    _raw_stream, _device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+    if _raw_stream is None:
+        _raw_stream, _device = (lambda _: torch.cuda.current_stream().cuda_stream), (lambda: 0)
+
+
 def _stream_handle():
     """The current stream of the current device, as a number (the Stream object that torch.cuda.current_stream makes on the way costs 3 us, a launch 4)."""
-    import torch
-    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    return raw(torch.cuda.current_device()) if raw else torch.cuda.current_stream().cuda_stream
+    if _raw_stream is None:
+        _torch_names()
+    return _raw_stream(_device())
 
 
 def _stream():
@@ -365,10 +378,12 @@ def _train_types(lib):
 
 
 def _dtype(x):
-    import torch
-    if x.dtype is torch.bfloat16:
+    if _f32 is None:
+        _torch_names()
+    t = x.dtype
+    if t is _bf16:
         return BF16
-    assert x.dtype is torch.float32, x.dtype
+    assert t is _f32, t
     return F32
 
 
@@ -391,18 +406,23 @@ def _flat(x, dtype=None):
     return x.data_ptr()
 
 
+def _flats(dtype, *tensors):
+    """_flat of each."""
+    return [x.data_ptr() if x is not None and x.dtype is dtype and x.is_contiguous() else _flat(x, dtype) for x in tensors]
+
+
 def _room(workspace):
     return (0, 0) if workspace is None else (_flat(workspace), workspace.nbytes)
 
 
 def _attn_shape(q, k, v, o, q_off, k_off, scale, lse=None, dout=None, grads=None):
-    import torch
-    T, i32 = q.dtype, torch.int32
+    dtype = _dtype(q)
+    T = q.dtype
     tq, nh, d = qs = q.shape
     tk, nkv, dk = ks = k.shape
     docs, = offs = q_off.shape
     assert T is k.dtype is v.dtype is o.dtype and ks == v.shape and qs == o.shape and d == dk, "shapes or types differ"
-    assert k_off.shape == offs and q_off.dtype is k_off.dtype is i32 and q_off.is_contiguous() and k_off.is_contiguous(), "int32 offsets, one more than documents"
+    assert k_off.shape == offs and q_off.dtype is k_off.dtype is _i32 and q_off.is_contiguous() and k_off.is_contiguous(), "int32 offsets, one more than documents"
     assert lse is None or lse.shape == (nh, tq), "lse is [heads, tokens]"
     so = _token_stride(o, tq, nh, d)
     if grads is None:
@@ -412,7 +432,7 @@ def _attn_shape(q, k, v, o, q_off, k_off, scale, lse=None, dout=None, grads=None
         dq, dk, dv = grads
         assert dq.shape == qs and dk.shape == ks == dv.shape and dq.dtype is dk.dtype is dv.dtype is T, "shapes or types differ"
         more = _token_stride(dq, tq, nh, d), _token_stride(dk, tk, nkv, d), _token_stride(dv, tk, nkv, d)
-    return _ATTN_SHAPE.pack(_dtype(q), nh, nkv, d, docs - 1, tq, tk, scale or 0.0, _token_stride(q, tq, nh, d), _token_stride(k, tk, nkv, d), _token_stride(v, tk, nkv, d), so,
+    return _ATTN_SHAPE.pack(dtype, nh, nkv, d, docs - 1, tq, tk, scale or 0.0, _token_stride(q, tq, nh, d), _token_stride(k, tk, nkv, d), _token_stride(v, tk, nkv, d), so,
                             *more, q_off.data_ptr(), k_off.data_ptr())
 
 
@@ -422,24 +442,21 @@ def attention_workspace_bytes(q, k, v, q_off, k_off, backward):
 
 def attention_forward(q, k, v, q_off, k_off, out, lse, workspace=None, scale=None):
     """q, out [tokens, heads, head_dim], k, v [tokens, kv heads, head_dim] (tokens may be strided), offsets int32 [documents + 1], lse [heads, tokens] fp32."""
-    import torch
     s = _attn_shape(q, k, v, out, q_off, k_off, scale, lse)
-    _check(load().br_attention_forward(s, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _flat(lse, torch.float32), *_room(workspace), _stream_handle()))
+    _check(load().br_attention_forward(s, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _flat(lse, _f32), *_room(workspace), _stream_handle()))
 
 
 def attention_backward(dout, q, k, v, out, lse, q_off, k_off, dq, dk, dv, workspace, scale=None):
     """dout laid out as out; dq, dk, dv may be strided (parts of one gradient)."""
-    import torch
     s = _attn_shape(q, k, v, out, q_off, k_off, scale, lse, dout, (dq, dk, dv))
-    _check(load().br_attention_backward(s, dout.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _flat(lse, torch.float32), dq.data_ptr(), dk.data_ptr(),
+    _check(load().br_attention_backward(s, dout.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _flat(lse, _f32), dq.data_ptr(), dk.data_ptr(),
                                         dv.data_ptr(), *_room(workspace), _stream_handle()))
 
 
 def _norm_shape(x, y, mods, shift_off, scale_off, row_off, group):
-    import torch
-    docs = group.shape[0]
-    assert x.shape == y.shape and docs == row_off.shape[0] - 1, "shapes differ"
-    return _NORM_SHAPE.pack(_dtype(y), *x.shape, docs, *mods.shape, shift_off, scale_off, _flat(row_off, torch.int32), _flat(group, torch.int32))
+    dtype, xs, (docs,) = _dtype(y), x.shape, group.shape
+    assert xs == y.shape and docs == row_off.shape[0] - 1, "shapes differ"
+    return _NORM_SHAPE.pack(dtype, *xs, docs, *mods.shape, shift_off, scale_off, *_flats(_i32, row_off, group))
 
 
 def layer_norm_workspace_bytes(x, dout, mods, shift_off, scale_off, row_off, group):
@@ -448,19 +465,17 @@ def layer_norm_workspace_bytes(x, dout, mods, shift_off, scale_off, row_off, gro
 
 def layer_norm_forward(x, mods, shift_off, scale_off, row_off, group, out, mean=None, rstd=None):
     """x [rows, hidden] fp32, mods [groups, stride] fp32, out [rows, hidden]; mean, rstd [rows] fp32 or both None."""
-    import torch
-    s, f = _norm_shape(x, out, mods, shift_off, scale_off, row_off, group), torch.float32
+    s = _norm_shape(x, out, mods, shift_off, scale_off, row_off, group)
     assert mean is None or mean.numel() == rstd.numel() == x.shape[0]
-    _check(load().br_layer_norm_forward(s, _flat(x, f), _flat(mods, f), _flat(out), _flat(mean, f), _flat(rstd, f), _stream_handle()))
+    px, pm, *stats = _flats(_f32, x, mods, mean, rstd)
+    _check(load().br_layer_norm_forward(s, px, pm, _flat(out), *stats, _stream_handle()))
 
 
 def layer_norm_backward(dout, x, mean, rstd, mods, shift_off, scale_off, row_off, group, residual, dx, dmods, workspace):
     """residual: the gradient that reaches x past the norm, or None; dx may be the same tensor."""
-    import torch
-    s, f = _norm_shape(x, dout, mods, shift_off, scale_off, row_off, group), torch.float32
+    s = _norm_shape(x, dout, mods, shift_off, scale_off, row_off, group)
     assert dx.shape == x.shape and dmods.shape == mods.shape and mean.numel() == rstd.numel() == x.shape[0] and (residual is None or residual.shape == x.shape)
-    _check(load().br_layer_norm_backward(s, _flat(dout), _flat(x, f), _flat(mean, f), _flat(rstd, f), _flat(mods, f), _flat(residual, f), _flat(dx, f), _flat(dmods, f), *_room(workspace),
-                                         _stream_handle()))
+    _check(load().br_layer_norm_backward(s, _flat(dout), *_flats(_f32, x, mean, rstd, mods, residual, dx, dmods), *_room(workspace), _stream_handle()))
 
 
 def edge_rows(tree, sched, D, edge_ids):
@@ -475,10 +490,11 @@ def edge_rows(tree, sched, D, edge_ids):
 
 
 def _edge_set(z_nodes, v_rows, edge_ids, row_parent, row_first, row_coef, clip_eps, n_total):
-    import torch
-    i32, (nodes, D), rows = torch.int32, z_nodes.shape, row_parent.shape[0]
+    if _f32 is None:
+        _torch_names()
+    (nodes, D), (rows,), (edges,) = z_nodes.shape, row_parent.shape, edge_ids.shape
     assert v_rows.shape == (rows, D) and row_first.shape[0] == rows + 1 and row_coef.numel() == 4 * rows, "shapes differ"
-    return _EDGE_SET.pack(D, nodes, rows, edge_ids.shape[0], n_total, clip_eps, _flat(edge_ids, i32), _flat(row_parent, i32), _flat(row_first, i32), _flat(row_coef, torch.float64))
+    return _EDGE_SET.pack(D, nodes, rows, edges, n_total, clip_eps, *_flats(_i32, edge_ids, row_parent, row_first), _flat(row_coef, _f64))
 
 
 def grpo_backward_workspace_bytes(z_nodes, v_rows, edge_ids, row_parent, row_first, row_coef):
@@ -487,11 +503,9 @@ def grpo_backward_workspace_bytes(z_nodes, v_rows, edge_ids, row_parent, row_fir
 
 def grpo_backward(z_nodes, v_rows, edge_ids, row_parent, row_first, row_coef, logp_old_nodes, adv_nodes, clip_eps, J, logp_new, grad_v, workspace, clipped=None, n_total=0):
     """Tables as edge_rows gives them, on the device; logp_new [edges], grad_v like v_rows, clipped uint8 [edges] or None."""
-    import torch
-    s, f = _edge_set(z_nodes, v_rows, edge_ids, row_parent, row_first, row_coef, clip_eps, n_total), torch.float32
+    s = _edge_set(z_nodes, v_rows, edge_ids, row_parent, row_first, row_coef, clip_eps, n_total)
     assert grad_v.shape == v_rows.shape and logp_new.shape == edge_ids.shape and logp_old_nodes.numel() == adv_nodes.numel() == z_nodes.shape[0], "shapes differ"
-    _check(load().br_grpo_backward(s, _flat(z_nodes, f), _flat(v_rows, f), _flat(logp_old_nodes, f), _flat(adv_nodes, f), _flat(J, f), _flat(logp_new, f), _flat(grad_v, f),
-                                   _flat(clipped), *_room(workspace), _stream_handle()))
+    _check(load().br_grpo_backward(s, *_flats(_f32, z_nodes, v_rows, logp_old_nodes, adv_nodes, J, logp_new, grad_v), _flat(clipped), *_room(workspace), _stream_handle()))
 
 
 class AdamwTensor(C.Structure):
