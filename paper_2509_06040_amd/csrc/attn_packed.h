@@ -125,8 +125,10 @@ inline br_status attn_grid(AttnArgs& a, int tokens, int heads, int rows, int par
 // 1800 keys, heads of 128 24 / 15.
 inline int attn_parts(const br_attn_shape& s, long long own_tokens, int own_heads, int own_rows, long long other_tokens, int heads, int per_cu, float step_us, int outputs) {
   if (own_tokens == 0 || other_tokens == 0 || s.n_docs == 0) return 1;
+  const int tiles = cdiv(cdiv(other_tokens, s.n_docs), 32);
+  if ((float)heads * tiles * step_us <= 7.f) return 1;  // (no number of parts can save 3 us)
   const long long blocks = std::max<long long>(cdiv(own_tokens, own_rows), std::min<long long>(s.n_docs, own_tokens)) * own_heads;
-  const int tiles = cdiv(cdiv(other_tokens, s.n_docs), 32), most = (int)std::min<long long>({(long long)per_cu * device_cu_count() / blocks, (long long)heads * tiles / 4, tiles, 64});
+  const int most = (int)std::min<long long>({(long long)per_cu * device_cu_count() / blocks, (long long)heads * tiles / 4, tiles, 64});
   int best = 1;
   float gain = 3.f;
   for (int n = 2; n <= most; ++n) {
