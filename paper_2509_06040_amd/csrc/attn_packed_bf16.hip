@@ -11,7 +11,8 @@
 // Bound by the matrix pipe, the exponentials issued beside it, and the clock that the chip's power leaves (2.0 to 2.3 GHz with random inputs; with inputs of zero
 // 20 to 30 % faster).  Measured: forward, 16 heads of 64, 16 documents of 1025 to 1101 tokens 96 us, 768 TFLOP/s (matrix pipe 32 % busy, VALU 54 %); backward of eight of them 155
 // us, 600 TFLOP/s by the formulas' five products, 840 by the seven; backward, 12 heads of 128, two documents of 4096 to 4608 728 us, 743 and 1041 (matrix pipe 51 % busy for
-// dq, 41 % for dk and dv, VALU 36 and 31 %).  A library product of 8192^3 reaches 1202 on the same card.
+// dq, 41 % for dk and dv, VALU 36 and 31 %); eight documents of 2001, 16 heads, forward 834 at heads of 64 and 1003 at 128, backward 1080 and
+// 1096 by the seven.  A library product of 8192^3 reaches 1202 on the same card.
 //
 // Tiles come straight from global memory into LDS, rows as they lie, 16-byte chunks permuted per row so that both the fragments of 16 rows
 // and the transposed reads (eight rows, two chunks) spread over the banks.
