@@ -5,7 +5,7 @@
 // (X - delta), and the products with the tile's rows, dk += Y1^T dS (dq the same) and dv += Y2^T P.  These wait for the next tile: between its scores' last
 // matrix instructions and theirs stand the exponentials of the tile itself.
 //
-// Both passes take scores anew from q, k and the log-sum-exp: seven products where the formulas have five, nothing of a tile's size in memory and every sum in one
+// Both kernels of the backward pass take scores anew from q, k and the log-sum-exp: seven products where the formulas have five, nothing of a tile's size in memory and every sum in one
 // wavefront's registers in a fixed order (dq added up over the workgroups of the keys instead would be 85 MB of fp32 for a head of a document of 4600 tokens).
 //
 // Bound by the matrix pipe, the exponentials issued beside it, and the clock that the chip's power leaves (2.0 to 2.3 GHz with random inputs; with inputs of zero
