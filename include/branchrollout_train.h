@@ -70,7 +70,8 @@ typedef struct {
   const int32_t* group;                /* dev [n_docs], each in [0, n_groups); the document is left alone otherwise */
 } br_norm_shape;
 
-size_t br_layer_norm_workspace_bytes(const br_norm_shape* shape); /* of the backward call */
+/* Of the backward call; at most 8 max(hidden, 64) (rows / 16 + 2 n_docs + 1024) bytes. */
+size_t br_layer_norm_workspace_bytes(const br_norm_shape* shape);
 
 /* x dev [rows, hidden] fp32; out dev out [rows, hidden]; mean, rstd dev out [rows] or both NULL. */
 br_status br_layer_norm_forward(const br_norm_shape* shape, const float* x, const float* mods, void* out,

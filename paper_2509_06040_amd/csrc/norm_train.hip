@@ -276,11 +276,11 @@ static void norm_form(int H, F f) {
 #undef BR_V
 }
 
-// Rows of a tile of the backward pass: as many workgroups as the units hold at once, four rows at least.
+// Rows of a tile of the backward pass: as many workgroups as the units hold at once, four rows at least, and no more column sums in the workspace than the header says.
 static int norm_tile(const br_norm_shape& s) {
   int per_cu = 1;
   norm_form(s.hidden, [&](auto Vc, auto Tc) { per_cu = NORM_PER_CU<decltype(Vc)::value, decltype(Tc)::value>; });
-  return std::max(4, cdiv(s.rows, (long long)per_cu * device_cu_count()));
+  return std::max({4, cdiv(s.rows, (long long)per_cu * device_cu_count()), cdiv(s.rows, s.rows / 16 + 960)});
 }
 
 size_t norm_train_workspace(const br_norm_shape& s) {
