@@ -577,19 +577,26 @@ static __device__ __forceinline__ void packed_grad_rows(const AttnArgs& a, const
       }
     };
     static_for<RA>([&](auto Nc) __attribute__((always_inline)) { fr[decltype(Nc)::value] = frag_of(Nc, 0, 0); });
-    int j = 0;
+    u32x4 there;  // ones where the lane's rows of a head's last tile are below the end
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+      const int row = (nt - 1) * PACK_TILE + (e >> 2) * 16 + 4 * g + (e & 3);
+      there[e >> 1] = (row < n_rows ? 0x0000FFFFu : 0u) | (row + 1 < n_rows ? 0xFFFF0000u : 0u);
+    }
+    int j = 0, left = nt;
     bool more = true;
     while (more) {
       static_for<NB>([&](auto Bc) __attribute__((always_inline)) {
         if (!more) return;
         constexpr int B = decltype(Bc)::value, P = B & 1;
         step(std::integral_constant<int, P>{}, Bc);
-        if (!KEYS && j == N - 1) {  // keys past the end
+        if (--left == 0) {  // a head's last tile: rows past the end (zeros, which an infinite own row makes scores of that are not numbers) count as none
+          left = nt;
 #pragma unroll
-          for (int qb = 0; qb < QB; ++qb)
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-              if (j * PACK_TILE + (e >> 2) * 16 + 4 * g + (e & 3) >= n_rows) df[P][qb][e >> 1] &= e & 1 ? 0x0000FFFFu : 0xFFFF0000u;
+          for (int qb = 0; qb < QB; ++qb) {
+            df[P][qb] &= there;
+            if constexpr (KEYS) pf[P][qb] &= there;
+          }
         }
         more = ++j < N;
         if (more) behind(Bc);

@@ -381,6 +381,7 @@ __global__ __launch_bounds__(256) void packed_attention_dkv_kernel(AttnArgs a) {
     L::put(lds + L::BYTES, nd);
     if (threadIdx.x < 2 * TILE_ROWS) refs[threadIdx.x] = next_ref;
     __syncthreads();
+    const int there = queries.end - q0;  // rows of the tile below the end; those past it (zeros, which an infinite key makes scores of that are not numbers) count as none
     q0 += TILE_ROWS;
     if (q0 >= queries.end) {
       q0 = queries.first;
@@ -402,8 +403,10 @@ __global__ __launch_bounds__(256) void packed_attention_dkv_kernel(AttnArgs a) {
       const f32x4 ref = *reinterpret_cast<const f32x4*>(refs + (b0 + b) * 16 + 4 * g), delta = *reinterpret_cast<const f32x4*>(refs + TILE_ROWS + (b0 + b) * 16 + 4 * g);
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        p[b][r] = __builtin_amdgcn_exp2f(fmaf(p[b][r], unit, -ref[r]));
-        ds[b][r] = p[b][r] * (ds[b][r] + delta[r]);
+        const float x = __builtin_amdgcn_exp2f(fmaf(p[b][r], unit, -ref[r]));
+        const bool in = (b0 + b) * 16 + 4 * g + r < there;
+        p[b][r] = in ? x : 0.f;
+        ds[b][r] = in ? x * (ds[b][r] + delta[r]) : 0.f;
       }
     }
 #pragma unroll

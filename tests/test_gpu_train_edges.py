@@ -1,0 +1,63 @@
+"""The training operators where inputs are not finite, matrices are wide, documents many: what the formulas say there, and refusals that only a device can show."""
+import os
+import sys
+
+import numpy as np
+import pytest
+import torch
+
+from gpu_util import DEV, bytes_buffer, dev, host
+from oracle import objective, train
+from paper_2509_06040_amd import binding as br
+from paper_2509_06040_amd import synth
+from test_gpu_train_ops import Packed, objective_case
+
+pytestmark = pytest.mark.gpu
+FORMS = [("bf16", 64), ("bf16", 128), ("f32", 16), ("f32", 64), ("f32", 128)]
+
+
+def off_by(got, ref):
+    return np.linalg.norm(got - ref) / np.linalg.norm(ref)
+
+
+# ------------------------------------------------------------------------------------------------------------ attention
+@pytest.mark.parametrize("dtype,d", FORMS)
+@pytest.mark.parametrize("heads,kv_heads,lq,lk", [(2, 2, (37,), (50,)), (2, 1, (64, 1), (20, 33)), (4, 2, (1201,), (70,)), (1, 1, (3, 130), (700, 5)), (8, 8, (2500,), (300,))])
+def test_keys_of_minus_infinity_have_gradients_of_zero(dtype, d, heads, kv_heads, lq, lk):
+    """Such keys count as none (probability 0): their dk and dv are 0, and those of the others are as without them, whatever the number of queries.  bf16 rounds the
+    terms of a sum twice (P or dS, and the output in dout . out) and the result once, by 0.00166 of a value each in the mean; errors of terms add up as the root of
+    their squares, which is above the sum itself where terms cancel; a fifth for the spread.  fp32: sums of up to 2500 terms, 2^-24 of their magnitudes each at most,
+    these 30 times the result: 1e-4 has a margin."""
+    p = Packed(dtype, d, heads, kv_heads, lq, lk, seed=d + lq[0], front=2, back=3)
+    p.q[:] = p.q.abs() + 0.01
+    none = np.arange(int(p.k_off[0]), int(p.k_off[-1]), 3)[1:]
+    p.k[torch.from_numpy(none).to(DEV)] = -float("inf")
+    p.forward()
+    p.backward()
+    dk, dv = host(p.dk), host(p.dv)
+    assert np.all(dk[none] == 0) and np.all(dv[none] == 0)
+    q, k, v, do = (host(t).astype(np.float64) for t in (p.q, p.k, p.v, p.dout))
+    there = np.setdiff1d(np.arange(len(k)), none)
+    k, v, k_off = k[there], v[there], np.searchsorted(there, p.k_off)
+    (_, rk, rv), _ = train.attention_grad(do, q, k, v, p.q_off, k_off, p.scale)
+    out, _, kept = train.attention(q, k, v, p.q_off, k_off, p.scale)
+    squares = np.zeros((2, *k.shape))
+    for a, b, x, y, h, pr in kept:
+        g = h // (heads // kv_heads)
+        ds = pr * (do[a:b, h] @ v[x:y, g].T - (do[a:b, h] * out[a:b, h]).sum(1, keepdims=True)) * p.scale
+        squares[0, x:y, g] += (ds ** 2).T @ q[a:b, h] ** 2
+        squares[1, x:y, g] += (pr ** 2).T @ do[a:b, h] ** 2
+    for got, ref, sq in ((dk, rk, squares[0]), (dv, rv, squares[1])):
+        bound = 1.2 * 0.00166 * np.sqrt(2 * sq.sum() + (ref ** 2).sum()) if dtype == "bf16" else 1e-4 * np.linalg.norm(ref)
+        assert np.linalg.norm(got[there] - ref) < bound
+
+
+@pytest.mark.parametrize("dtype,d", FORMS)
+@pytest.mark.parametrize("lq", [(1,), (45,), (300,)])
+def test_documents_whose_keys_are_all_minus_infinity_have_no_gradients(dtype, d, lq):
+    p = Packed(dtype, d, 2, 1, lq, (77,), seed=2)
+    p.q[:] = p.q.abs() + 0.01
+    p.k[:] = -float("inf")
+    p.forward()
+    p.backward()
+    assert np.all(host(p.out) == 0) and np.all(host(p.dk) == 0) and np.all(host(p.dv) == 0)
