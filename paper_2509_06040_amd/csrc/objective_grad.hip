@@ -103,10 +103,10 @@ __device__ inline ObjTerm obj_term(const br_edge_set& s, double squares, double 
   ObjTerm t;
   t.logp = c0 - h * squares;
   const double rho = exp(t.logp - (double)logp_old), a = adv, eps = s.clip_eps;
-  const double held = fmin(fmax(rho, 1.0 - eps), 1.0 + eps) * a;
-  t.clipped = held < rho * a;
-  t.term = fmin(rho * a, held) * inv_n;
-  t.weight = t.clipped ? 0.0 : -rho * a * inv_n;
+  const double term = rho * a, held = fmin(fmax(rho, 1.0 - eps), 1.0 + eps) * a;
+  t.clipped = held < term;
+  t.term = (t.clipped ? held : term) * inv_n;  // (not their minimum, which drops a term that is not a number)
+  t.weight = t.clipped ? 0.0 : -term * inv_n;
   return t;
 }
 

@@ -61,3 +61,18 @@ def test_documents_whose_keys_are_all_minus_infinity_have_no_gradients(dtype, d,
     p.forward()
     p.backward()
     assert np.all(host(p.out) == 0) and np.all(host(p.dk) == 0) and np.all(host(p.dv) == 0)
+
+
+# ------------------------------------------------------------------------------------------------------------ objective
+@pytest.mark.parametrize("T,splits,K,trees,D", [(8, (2, 4), 2, 1, 64), (8, (2, 4), 2, 2, 8192)])
+def test_a_velocity_that_is_not_a_number_shows_in_the_objective(T, splits, K, trees, D):
+    """One launch or two: J, the row's log-densities and its gradient are NaN, the other rows' are as they were."""
+    c = objective_case(T, splits, K, trees, D, 0.9, True, 0.2, seed=D, moved=0.02)
+    c["vd"][1, 5] = float("nan")
+    J, new, grad, clipped = torch.zeros(1, device=DEV), torch.empty(c["E"], device=DEV), torch.empty_like(c["vd"]), torch.full((c["E"],), 7, dtype=torch.uint8, device=DEV)
+    br.grpo_backward(c["zd"], c["vd"], *c["tables"], dev(c["old"]), dev(c["advn"]), c["clip"], J, new, grad, c["ws"], clipped=clipped)
+    hit = np.arange(c["first"][1], c["first"][2])
+    rest = np.delete(np.arange(c["R"]), 1)
+    assert np.isnan(host(new)[hit]).all() and np.isfinite(np.delete(host(new), hit)).all() and np.all(host(clipped)[hit] == 0)
+    assert np.isnan(host(grad)[1]).all() and np.array_equal(host(grad)[rest], c["grad"][rest])
+    assert np.isnan(host(J)[0])
