@@ -604,8 +604,9 @@ __global__ __launch_bounds__(256) void grpo_objective_kernel(const float* __rest
     const int g = ids[e];
     const double rho = exp((double)logp_new[e] - (double)logp_old[g]), a = adv[g];
     const double cl = fmin(fmax(rho, 1.0 - clip_eps), 1.0 + clip_eps);
-    acc += fmin(rho * a, cl * a);
-    if (clipped) clipped[e] = cl * a < rho * a ? 1 : 0;  // the clipped term is the one taken
+    const bool held = cl * a < rho * a;  // the clipped term is the one taken (not their minimum, which drops a term that is not a number)
+    acc += held ? cl * a : rho * a;
+    if (clipped) clipped[e] = held ? 1 : 0;
   }
   acc = wsum_d(acc);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = acc;

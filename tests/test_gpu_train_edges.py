@@ -76,3 +76,14 @@ def test_a_velocity_that_is_not_a_number_shows_in_the_objective(T, splits, K, tr
     assert np.isnan(host(new)[hit]).all() and np.isfinite(np.delete(host(new), hit)).all() and np.all(host(clipped)[hit] == 0)
     assert np.isnan(host(grad)[1]).all() and np.array_equal(host(grad)[rest], c["grad"][rest])
     assert np.isnan(host(J)[0])
+
+
+def test_a_log_density_that_is_not_a_number_shows_in_the_objectives_value():
+    n = 300
+    r = np.random.default_rng(0)
+    new, old, adv = (r.standard_normal(n).astype(np.float32) for _ in range(3))
+    new[17] = np.nan
+    J, clipped = torch.zeros(1, device=DEV), torch.full((n,), 7, dtype=torch.uint8, device=DEV)
+    br.grpo_objective(dev(new), dev(old), dev(adv), dev(np.arange(n, dtype=np.int32)), n, 0.2, J, clipped)
+    ref, marks = objective.grpo_objective(new, old, adv, float(np.float32(0.2)))
+    assert np.isnan(ref) and np.isnan(host(J)[0]) and np.array_equal(host(clipped).astype(bool), marks)
