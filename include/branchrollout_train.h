@@ -156,7 +156,9 @@ typedef struct {
   const float* grad_scale;             /* dev [1] or NULL: a factor of every gradient (clipping by a norm, loss scaling) */
 } br_adamw_cfg;
 
-/* tensors host [n_tensors]; one launch for 48 of them. */
+/* tensors host [n_tensors]; one launch for 48 of them.
+ * The step's number, learning rate and corrections travel with the launch: a graph that has captured a call (states in 32 bits) takes the same step
+ * again on every replay, reading gradients and *grad_scale anew.  States in 8 bits cannot be captured (BR_EINVAL): replays would draw the same random bits. */
 br_status br_adamw_step(const br_adamw_cfg* cfg, const br_adamw_tensor* tensors, int32_t n_tensors, void* stream);
 
 /* The values that 8-bit states stand for (m, and the second moment v itself), as 32-bit states hold them: for checkpoints

@@ -539,7 +539,8 @@ class AdamW:
         self.cfg = AdamwCfg(lr, betas[0], betas[1], eps, step, seed, _dtype(grads[0]) if n else F32, bits, None)
 
     def step(self, lr=None, grad_scale=None):
-        """One step; grad_scale: a device tensor of one fp32 factor of all gradients, or None."""
+        """One step; grad_scale: a device tensor of one fp32 factor of all gradients, or None.  Captured in a graph (32-bit states only) it is this same step, with its
+        number and learning rate, on every replay."""
         if lr is not None:
             self.cfg.lr = lr
         self.cfg.step += 1

@@ -164,6 +164,11 @@ extern "C" br_status br_adamw_step(const br_adamw_cfg* c, const br_adamw_tensor*
   BR_REQUIRE(c->state_bits == 32 || c->state_bits == 8, BR_EINVAL, "br_adamw_step: state_bits is 32 or 8");
   BR_REQUIRE(c->step >= 1 && c->beta1 >= 0 && c->beta1 < 1 && c->beta2 >= 0 && c->beta2 < 1 && c->eps >= 0 && isfinite(c->eps) && isfinite(c->lr), BR_EINVAL,
              "br_adamw_step: step starts at 1, 0 <= beta < 1, eps >= 0, lr finite");
+  if (c->state_bits == 8) {
+    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+    if (hipStreamIsCapturing((hipStream_t)stream, &capture) != hipSuccess) (void)hipGetLastError();  // (no device here, or a stream that the launch itself will refuse)
+    BR_REQUIRE(capture == hipStreamCaptureStatusNone, BR_EINVAL, "br_adamw_step: a captured step would draw the same random bits on every replay: states in 8 bits cannot be captured");
+  }
   for (int i = 0; i < n; ++i) {
     BR_REQUIRE(t[i].n >= 0 && isfinite(t[i].weight_decay), BR_EINVAL, "br_adamw_step: negative size or weight decay that is not finite");
     BR_REQUIRE(t[i].n < (1LL << 34), BR_ESHAPE, "br_adamw_step: more than 2^34 elements in a tensor");

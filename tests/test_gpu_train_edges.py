@@ -87,3 +87,29 @@ def test_a_log_density_that_is_not_a_number_shows_in_the_objectives_value():
     br.grpo_objective(dev(new), dev(old), dev(adv), dev(np.arange(n, dtype=np.int32)), n, 0.2, J, clipped)
     ref, marks = objective.grpo_objective(new, old, adv, float(np.float32(0.2)))
     assert np.isnan(ref) and np.isnan(host(J)[0]) and np.array_equal(host(clipped).astype(bool), marks)
+
+
+# ---------------------------------------------------------------------------------------------------------------- AdamW
+def test_adamw_refuses_to_have_its_random_rounding_captured():
+    """A replay would draw the captured step's random bits again: elements with low ones would never reach the next code."""
+    n = 1000
+    p, g = torch.ones(n, device=DEV), torch.full((n,), 0.01, device=DEV)
+    m, v, ms, vs = (torch.zeros(k, dtype=t, device=DEV) for k, t in ((n, torch.uint8), (n, torch.uint8), (4, torch.float32), (4, torch.float32)))
+    opt = br.AdamW([p], [g], [m], [v], [ms], [vs])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        g.add_(0.01)
+        with pytest.raises(br.BranchRolloutError) as e:
+            opt.step()
+    assert e.value.code == -1 and "captur" in str(e.value) and opt.cfg.step == 0
+    graph.replay()
+    torch.cuda.synchronize()
+    assert np.all(host(p) == 1) and np.all(host(m) == 0)
+    opt.step()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        opt.step()
+    side.synchronize()
+    assert opt.cfg.step == 2 and np.all(host(p) < 1) and np.any(host(m) != 0)
