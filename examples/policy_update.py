@@ -80,17 +80,17 @@ class Policy:
             self.W[n].grad = torch.zeros_like(self.W[n])
         self.optimizers = []
         for dtype in sorted({self.W[n].dtype for n in self.names}, key=str):  # (gradients of a handle are of one type)
-            w = [self.W[n].detach() for n in self.names if self.W[n].dtype == dtype]
+            w = [self.W[n] for n in self.names if self.W[n].dtype == dtype]
             g = [self.W[n].grad for n in self.names if self.W[n].dtype == dtype]
             matrix = [n.endswith("_w") for n in self.names if self.W[n].dtype == dtype]
             kw = {}
             if dtype == torch.bfloat16:
-                kw["copies"], w = w, [x.float() for x in w]
+                kw["copies"], w = w, [x.detach().float() for x in w]
             if state_bits == 8:
                 m, v = ([torch.zeros(x.numel(), dtype=torch.uint8, device=device) for x in w] for _ in range(2))
                 kw["m_scales"], kw["v_scales"] = ([torch.zeros((x.numel() + 255) // 256, device=device) for x in w] for _ in range(2))
             else:
-                m, v = ([torch.zeros_like(x) for x in w] for _ in range(2))
+                m, v = ([torch.zeros_like(x, requires_grad=False) for x in w] for _ in range(2))
             self.optimizers.append(br.AdamW(w, g, m, v, weight_decay=[0.01 if x else 0.0 for x in matrix], lr=lr, seed=seed, **kw))
 
     def velocity(self, z, t, cond):

@@ -519,7 +519,10 @@ class AdamwCfg(C.Structure):
 
 class AdamW:
     """The tensors of a network and their optimizer states (lists of equal length; every tensor contiguous).  params fp32; grads all fp32 or all bf16; m, v
-    fp32, or uint8 codes with m_scales, v_scales (fp32, one of 256 elements); copies: bf16 tensors that receive the rounded parameters, or None."""
+    fp32, or uint8 codes with m_scales, v_scales (fp32, one of 256 elements); copies: bf16 tensors that receive the rounded parameters, or None.
+
+    The tensors' addresses are taken once: gradients have to stay the same tensors (zero them in place; zero_grad(set_to_none=True) makes others).  Where a gradient
+    is the .grad of its parameter or of its copy, step() raises ValueError if that has been replaced."""
 
     def __init__(self, params, grads, m, v, m_scales=None, v_scales=None, copies=None, weight_decay=0.01, lr=1e-4, betas=(0.9, 0.999), eps=1e-8, seed=0, step=0):
         import torch
@@ -529,18 +532,22 @@ class AdamW:
         state = torch.float32 if bits == 32 else torch.uint8
         decay = [weight_decay] * n if isinstance(weight_decay, (int, float)) else list(weight_decay)
         self.tensors = (AdamwTensor * max(n, 1))()
-        self.n, self._keep = n, (params, grads, m, v, m_scales, v_scales, copies)
+        self.n, self._leaves, self._keep = n, [], (params, grads, m, v, m_scales, v_scales, copies)
         f = torch.float32
         for i, (p, g, mm, vv, ms, vs, c, w) in enumerate(zip(params, grads, m, v, m_scales or none, v_scales or none, copies or none, decay, strict=True)):
             k = p.numel()
             assert g.numel() == mm.numel() == vv.numel() == k and (c is None or c.numel() == k) and (ms is None or ms.numel() == vs.numel() == (k + 255) // 256), "sizes differ"
             assert g.dtype == grads[0].dtype
+            self._leaves += [(x, g) for x in (p, c) if x is not None and x.is_leaf and x.grad is g]
             self.tensors[i] = AdamwTensor(_flat(p, f), _flat(g), _flat(mm, state), _flat(vv, state), _flat(ms, f), _flat(vs, f), _flat(c, torch.bfloat16), k, w)
         self.cfg = AdamwCfg(lr, betas[0], betas[1], eps, step, seed, _dtype(grads[0]) if n else F32, bits, None)
 
     def step(self, lr=None, grad_scale=None):
         """One step; grad_scale: a device tensor of one fp32 factor of all gradients, or None.  Captured in a graph (32-bit states only) it is this same step, with its
         number and learning rate, on every replay."""
+        for x, g in self._leaves:
+            if x.grad is not g:
+                raise ValueError("a gradient is another tensor than the one that this optimizer was given")
         if lr is not None:
             self.cfg.lr = lr
         self.cfg.step += 1
