@@ -94,14 +94,14 @@ def _h(a, dtype):
     return a, a.ctypes.data_as(C.c_void_p)
 
 
-_f32 = _bf16 = _i32 = _f64 = _raw_stream = _device = None
+_f32 = _bf16 = _i32 = _f64 = _u8 = _raw_stream = _device = None
 
 
 def _torch_names():
     """What the calls below need of torch, once: a call of small tensors is the host's time, and an import statement and a lookup in it are 0.1 us each."""
-    global _f32, _bf16, _i32, _f64, _raw_stream, _device
+    global _f32, _bf16, _i32, _f64, _u8, _raw_stream, _device
     import torch
-    _f32, _bf16, _i32, _f64 = torch.float32, torch.bfloat16, torch.int32, torch.float64
+    _f32, _bf16, _i32, _f64, _u8 = torch.float32, torch.bfloat16, torch.int32, torch.float64, torch.uint8
     _raw_stream, _device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
     if _raw_stream is None:
         _raw_stream, _device = (lambda _: torch.cuda.current_stream().cuda_stream), (lambda: 0)
@@ -504,8 +504,9 @@ def grpo_backward_workspace_bytes(z_nodes, v_rows, edge_ids, row_parent, row_fir
 def grpo_backward(z_nodes, v_rows, edge_ids, row_parent, row_first, row_coef, logp_old_nodes, adv_nodes, clip_eps, J, logp_new, grad_v, workspace, clipped=None, n_total=0):
     """Tables as edge_rows gives them, on the device; logp_new [edges], grad_v like v_rows, clipped uint8 [edges] or None."""
     s = _edge_set(z_nodes, v_rows, edge_ids, row_parent, row_first, row_coef, clip_eps, n_total)
-    assert grad_v.shape == v_rows.shape and logp_new.shape == edge_ids.shape and logp_old_nodes.numel() == adv_nodes.numel() == z_nodes.shape[0], "shapes differ"
-    _check(load().br_grpo_backward(s, *_flats(_f32, z_nodes, v_rows, logp_old_nodes, adv_nodes, J, logp_new, grad_v), _flat(clipped), *_room(workspace), _stream_handle()))
+    assert grad_v.shape == v_rows.shape and logp_new.shape == edge_ids.shape and logp_old_nodes.numel() == adv_nodes.numel() == z_nodes.shape[0] and J.numel() == 1, "shapes differ"
+    assert clipped is None or clipped.shape == edge_ids.shape, "clipped is [edges]"
+    _check(load().br_grpo_backward(s, *_flats(_f32, z_nodes, v_rows, logp_old_nodes, adv_nodes, J, logp_new, grad_v), _flat(clipped, _u8), *_room(workspace), _stream_handle()))
 
 
 class AdamwTensor(C.Structure):
@@ -548,11 +549,13 @@ class AdamW:
         for x, g in self._leaves:
             if x.grad is not g:
                 raise ValueError("a gradient is another tensor than the one that this optimizer was given")
+        assert grad_scale is None or grad_scale.numel() == 1, "grad_scale is one value"
+        scale, stream = _flat(grad_scale, _f32), _stream()
         if lr is not None:
             self.cfg.lr = lr
         self.cfg.step += 1
-        self.cfg.grad_scale = None if grad_scale is None else _p(grad_scale).value
-        code = load().br_adamw_step(C.byref(self.cfg), self.tensors, C.c_int32(self.n), _stream())
+        self.cfg.grad_scale = scale
+        code = load().br_adamw_step(C.byref(self.cfg), self.tensors, C.c_int32(self.n), stream)
         if code != 0:
             self.cfg.step -= 1
         _check(code)
