@@ -10,6 +10,7 @@ import sys
 
 import torch
 import torch.nn.functional as F
+from torch.autograd.function import once_differentiable
 
 sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 from paper_2509_06040_amd import binding as br  # noqa: E402
@@ -34,6 +35,7 @@ class Attention(torch.autograd.Function):
         return out
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dout):
         qkv, off, out, lse = ctx.saved_tensors
         (q, k, v), dqkv = qkv.unbind(1), torch.empty_like(qkv)
@@ -57,6 +59,7 @@ class Norm(torch.autograd.Function):
         return out, x.view_as(x)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dout, dx):
         x, mods, mean, rstd, off, group = ctx.saved_tensors
         rows = mods.flatten(1)

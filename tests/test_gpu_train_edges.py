@@ -113,3 +113,17 @@ def test_adamw_refuses_to_have_its_random_rounding_captured():
         opt.step()
     side.synchronize()
     assert opt.cfg.step == 2 and np.all(host(p) < 1) and np.any(host(m) != 0)
+
+
+# -------------------------------------------------------------------------------------------------------------- example
+def test_second_derivatives_are_refused():
+    sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+    import policy_update as example
+    off, group = dev(np.array([0, 20, 32], np.int32)), dev(np.array([0, 1], np.int32))
+    qkv = torch.randn(32, 3, 2, 16, device=DEV, requires_grad=True)
+    x, mods = torch.randn(32, 64, device=DEV, requires_grad=True), torch.randn(2, 2, 64, device=DEV, requires_grad=True)
+    for out, leaf in ((example.Attention.apply(qkv, off), qkv), (example.Norm.apply(x, mods, 0, 1, off, group, torch.float32)[0], x)):
+        out = out.square().sum()
+        first, = torch.autograd.grad(out, leaf, create_graph=True)
+        with pytest.raises(RuntimeError, match="differentiate twice"):
+            (out + first.square().sum()).backward()
