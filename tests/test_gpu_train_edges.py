@@ -127,3 +127,58 @@ def test_second_derivatives_are_refused():
         first, = torch.autograd.grad(out, leaf, create_graph=True)
         with pytest.raises(RuntimeError, match="differentiate twice"):
             (out + first.square().sum()).backward()
+
+
+# ---------------------------------------------------------------------------------------------- matrices of 4 GiB and more
+class Wide(Packed):
+    """Queries, keys, values, output and all gradients as columns of one matrix whose tokens lie `stride` elements apart."""
+
+    def __init__(self, d, heads, kv_heads, lens, stride, seed=0):
+        super().__init__("bf16", d, heads, kv_heads, lens, lens, seed=seed)
+        T, at, whole = int(self.q_off[-1]), [0], torch.empty(int(self.q_off[-1]) * stride, dtype=torch.bfloat16, device=DEV)
+
+        def column(x):
+            n = x.shape[1]
+            t = whole.as_strided((T, n, d), (stride, d, 1), at[0])
+            t.copy_(x)
+            at[0] += n * d
+            return t
+        for name in ("q", "k", "v", "out", "dout", "dq", "dk", "dv"):
+            setattr(self, name, column(getattr(self, name)))
+        self.whole = ()
+        self.work = bytes_buffer(max(br.attention_workspace_bytes(self.q, self.k, self.v, self.qo, self.ko, b) for b in (False, True)))
+
+
+@pytest.mark.parametrize("d,heads,kv_heads", [(64, 2, 2), (128, 2, 1)])
+@pytest.mark.parametrize("lens", [(63,), (64,), (33, 0, 31), (1, 70, 60)])
+def test_attention_over_matrices_around_4_gib(d, heads, kv_heads, lens):
+    """Tokens 64 MiB apart: 63 of them end below 2^32 bytes, 64 do not."""
+    Wide(d, heads, kv_heads, lens, 1 << 25, seed=d).run()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("most", [2, 4, 9, 33])
+def test_gradients_of_short_documents_of_matrices_past_4_gib_carry_two_roundings(d, most):
+    """As in matrices below 4 GiB: 0.00166 sqrt(2) = 0.00235 of the norm; the output's own rounding must not come on top."""
+    r = np.random.default_rng(most)
+    lens = [int(n) for n in r.integers(2, most + 1, 60)]
+    p = Wide(d, 4, 4, lens, ((1 << 31) // sum(lens) // 4096 + 1) * 4096, seed=d + most).run()
+    span = p.q.stride(0) * p.q.shape[0] * 2
+    assert span >= 1 << 32
+    q, k, v, do = (host(t) for t in (p.q, p.k, p.v, p.dout))
+    refs, _ = train.attention_grad(do, q, k, v, p.q_off, p.k_off, p.scale)
+    for t, ref in zip((p.dq, p.dk, p.dv), refs):
+        assert off_by(host(t), ref) < 0.0027
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_keys_of_minus_infinity_in_matrices_past_4_gib(d):
+    p = Wide(d, 2, 1, (70, 31), 1 << 25, seed=3)
+    p.q[:] = p.q.abs() + 0.01
+    p.k[::5] = -float("inf")
+    p.forward()
+    p.backward()
+    none = np.arange(101) % 5 == 0
+    for t in (p.dk, p.dv):
+        assert np.all(host(t)[none] == 0) and np.all(np.isfinite(host(t))) and np.all(host(t)[~none].any((1, 2)))
+    assert np.isfinite(host(p.out)).all()
