@@ -44,14 +44,7 @@ __device__ inline void row_sums(float* a, float* b, float* red, int turn) {
 
 // Group of the document that holds `row` (-1: none), and the first row behind that document.
 __device__ inline int row_group(const br_norm_shape& s, int row, int* end) {
-  const int lane = threadIdx.x & 63;
-  int before = 0;  // offsets up to `row`
-  for (int base = 0; base <= s.n_docs; base += 64) {
-    const int i = base + lane;
-    const unsigned long long m = __builtin_amdgcn_ballot_w64(i <= s.n_docs && s.row_off[min(i, s.n_docs)] <= row);
-    before += __builtin_popcountll(m);
-    if (m != ~0ull) break;
-  }
+  const int before = leading(s.n_docs + 1, [&](int i) { return s.row_off[i] <= row; });  // offsets up to `row`
   const int next = before <= s.n_docs ? s.row_off[before] : s.rows;
   *end = min(max(next, row + 1), s.rows);
   const int g = before >= 1 && before <= s.n_docs ? s.group[before - 1] : -1;

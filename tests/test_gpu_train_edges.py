@@ -10,7 +10,7 @@ from gpu_util import DEV, bytes_buffer, dev, host
 from oracle import objective, train
 from paper_2509_06040_amd import binding as br
 from paper_2509_06040_amd import synth
-from test_gpu_train_ops import Packed, objective_case
+from test_gpu_train_ops import Packed, norm_case, objective_case
 
 pytestmark = pytest.mark.gpu
 FORMS = [("bf16", 64), ("bf16", 128), ("f32", 16), ("f32", 64), ("f32", 128)]
@@ -182,3 +182,73 @@ def test_keys_of_minus_infinity_in_matrices_past_4_gib(d):
     for t in (p.dk, p.dv):
         assert np.all(host(t)[none] == 0) and np.all(np.isfinite(host(t))) and np.all(host(t)[~none].any((1, 2)))
     assert np.isfinite(host(p.out)).all()
+
+
+# ------------------------------------------------------------------------------------------------------- many documents
+def lengths(n, seed):
+    """Mostly some tokens, many documents without any, a few of several tiles."""
+    r = np.random.default_rng(seed)
+    lens = r.integers(0, 6, n)
+    lens[r.integers(0, n, 5)] = [130, 64, 257, 128, 65]
+    return [int(x) for x in lens]
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 128), ("f32", 16)])
+@pytest.mark.parametrize("heads,kv_heads", [(1, 1), (6, 2)])
+def test_attention_over_thousands_of_documents(dtype, d, heads, kv_heads):
+    """More than are counted one by one: places of a search, some of which hold no tile."""
+    Packed(dtype, d, heads, kv_heads, lengths(1500, d), lengths(1500, d + heads), seed=d, front=150, back=70).run()
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("f32", 16)])
+@pytest.mark.parametrize("n,length", [(1022, 128), (1023, 128), (1200, 64)])
+def test_attention_over_documents_as_long_as_a_tile(dtype, d, n, length):
+    """On both sides of that number: equal documents, whose softmax is checked for a few of them (all others are the same ones again)."""
+    few = 7
+    q, k, v, do = (torch.randn(few * length, 1, d, device=DEV).to(torch.bfloat16 if dtype == "bf16" else torch.float32) for _ in range(4))
+    reps = -(-n // few)
+    many = [x.view(few, length, 1, d).repeat(reps, 1, 1, 1)[:n].reshape(n * length, 1, d) for x in (q, k, v, do)]
+
+    def both(q, k, v, do, docs):
+        off = dev(np.arange(docs + 1, dtype=np.int32) * length)
+        out, lse, grads = torch.empty_like(q), torch.empty(1, docs * length, device=DEV), [torch.full_like(q, 7.0) for _ in range(3)]
+        ws = bytes_buffer(max(br.attention_workspace_bytes(q, k, v, off, off, b) for b in (False, True)))
+        br.attention_forward(q, k, v, off, off, out, lse, ws)
+        br.attention_backward(do, q, k, v, out, lse, off, off, *grads, ws)
+        return [host(x).reshape(docs, length, -1) for x in (out, lse, *grads)]
+    for got, ref in zip(both(*many, n), both(q, k, v, do, few)):
+        bound = 2.0 ** -7 if dtype == "bf16" else 1e-4  # (the few may be cut in parts: another order of sums; one rounding to bf16 more)
+        assert np.abs(got - np.tile(ref, (reps, 1, 1))[:n]).max() <= bound * np.abs(ref).max()
+
+
+def test_a_hundred_thousand_documents_of_one_token():
+    """A softmax over one key: the output is its value, the log-sum-exp its score, only v has a gradient.  A workgroup's time must not grow with the documents."""
+    n, d = 100_000, 16
+    q, k, v, do = (torch.randn(n, 1, d, device=DEV) for _ in range(4))
+    off, out, lse, grads = dev(np.arange(n + 1, dtype=np.int32)), torch.empty_like(q), torch.empty(1, n, device=DEV), [torch.full_like(q, 7.0) for _ in range(3)]
+    ws = bytes_buffer(max(br.attention_workspace_bytes(q, k, v, off, off, b) for b in (False, True)))
+    br.attention_forward(q, k, v, off, off, out, lse, ws)
+    br.attention_backward(do, q, k, v, out, lse, off, off, *grads, ws)
+    score = (host(q).astype(np.float64) * host(k)).sum((1, 2)) / 4
+    assert np.abs(host(out) - host(v)).max() < 1e-6 and np.abs(host(lse)[0] - score).max() < 1e-5
+    # p is 1 to 2^-20 (fp32 roundings of a score of at most 10 in powers of two); dS is p times a difference of two equal sums of 16 products
+    size = np.abs(host(do) * host(v)).sum((1, 2)).max()
+    assert np.abs(host(grads[2]) - host(do)).max() < 1e-5 and max(np.abs(host(g)).max() for g in grads[:2]) < 1e-5 * size
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_layer_norm_over_thousands_of_documents(dtype):
+    lens = lengths(3000, 1)
+    norm_case(dtype, 64, lens, [int(g) for g in np.random.default_rng(2).integers(-1, 9, 3000)], seed=3, front=9, back=30)
+
+
+def test_offsets_of_thousands_of_documents_in_no_order_stay_inside():
+    """Offsets that do not ascend name no documents, but no row outside the matrices is written either, and what lies around them is as it was."""
+    n, T, d = 2000, 400, 16
+    off = dev(np.random.default_rng(0).integers(-50, T + 50, n + 1).astype(np.int32))
+    big = torch.full((7, T + 64, 1, d), 7.0, device=DEV)
+    q, k, v, out, dq, dk, dv = big[:, 32:32 + T].unbind(0)
+    lse, ws = torch.full((1, T), 7.0, device=DEV), bytes_buffer(max(br.attention_workspace_bytes(q, k, v, off, off, b) for b in (False, True)))
+    br.attention_forward(q, k, v, off, off, out, lse, ws)
+    br.attention_backward(out, q, k, v, out, lse, off, off, dq, dk, dv, ws)
+    assert np.all(host(big[:, :32]) == 7.0) and np.all(host(big[:, 32 + T:]) == 7.0) and np.all(host(big[:3]) == 7.0)
