@@ -60,7 +60,8 @@ br_status br_attention_backward(const br_attn_shape* shape, const void* dout, co
  *   y[r] = (x[r] - mean[r]) rstd[r],  out[r] = y[r] (1 + scale[g]) + shift[g],  g = group[document of r]
  * shift and scale of group g are mods + g*mods_stride + {shift_off, scale_off}, hidden values each.  With one group
  * this is the LayerNorm with weight 1 + scale and bias shift.  Rows of no document are left alone.
- * BR_ESHAPE unless hidden, mods_stride and the offsets are multiples of 4 and pointers 16-byte aligned; hidden <= 16384.
+ * BR_ESHAPE unless hidden, mods_stride and the offsets are multiples of 4 and pointers 16-byte aligned; hidden <= 16384,
+ * n_groups <= 65535, backward n_groups (n_docs + 2050) <= 2^28.
  * ------------------------------------------------------------------------- */
 typedef struct {
   int32_t dtype;                       /* of out and dout; everything else is fp32 */

@@ -55,3 +55,14 @@ def test_workspaces_of_the_performance_cases_fit_what_these_allocate():
             s = br.EdgeSet(c["D"], nodes, len(rows), len(edges), 0, 0.1, P.value, P.value, P.value, P.value)
             assert 0 < br.load().br_grpo_backward_workspace_bytes(C.byref(s)) <= 8 * (len(edges) * (c["D"] // 1024 + 2) + 1024), c
     assert {"norm", "attention", "objective"} <= seen
+
+
+@pytest.mark.parametrize("groups,docs,ok", [(65535, 2046, True), (65535, 2047, False), (15360, 15360, True), (16384, 16384, False), (1, 1 << 24, True), (17, 1 << 24, False)])
+def test_layer_norm_backward_refuses_groups_times_documents_that_would_take_seconds(groups, docs, ok):
+    """The join reads every tile once for each group; forward has no such join."""
+    s = br.NormShape(br.BF16, 1 << 20, 64, docs, groups, 128, 0, 64, P.value, P.value)
+    lib = br.load()
+    assert (lib.br_layer_norm_workspace_bytes(C.byref(s)) > 0) == ok
+    if not ok:
+        assert lib.br_layer_norm_backward(C.byref(s), P, P, P, P, P, None, P, P, P, C.c_size_t(1 << 50), None) == -3
+        assert b"br_layer_norm_backward" in lib.br_last_error() and b"groups" in lib.br_last_error()
