@@ -101,5 +101,12 @@ inline void f32_ring_tile(int M, int N, int K, int rps, int units, int* rb, int*
     }
 }
 
+// Objective's gradient: whether one workgroup of 16 wavefronts, an edge, then a row, each, does all of a small set in one launch.  The two launches of larger sets are 5 to 6 us of the
+// device and 11.5 to 12.3 of a caller's stream of calls, one launch 8.5 there until its own time is more.  us of such a stream, two launches / one: 1 edge, 256 values 11.3 / 8.7, 2048
+// 11.5 / 8.7, 4096 11.5 / 11.7, 32 768 11.2 / 72; 10, 2392 values 12.2 / 10.9; 16, 1024 11.5 / 8.6, 2048 11.5 / 11.4; 21, 716 12.3 / 9.2; 32, 256 11.5 / 8.5, 1024 11.4 / 11.6; 64, 64
+// 11.6 / 11.6; 128, 256 11.6 / 20.7.  Replayed in a graph, where the host costs nothing: 8 edges, 256 values 5.5 / 4.2; 16, 1024 5.7 / 7.9; 32, 256 5.7 / 7.4.
+constexpr int OBJECTIVE_SMALL_EDGES = 32;
+inline bool objective_one_launch(int edges, long long D) { return edges <= OBJECTIVE_SMALL_EDGES && D <= 2560 && edges * D <= 24576; }
+
 }  // namespace rule
 }  // namespace br

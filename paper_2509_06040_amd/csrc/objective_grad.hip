@@ -5,6 +5,7 @@
 // first read, for edges that are not clipped; up to 256 MB of it comes out of the memory-side cache.
 // Measured: four trees of 16 leaves, latents of 65 536, half of the edges kept: 40 us for the squares (172 MB, 4.3 TB/s), 27 for the gradient (169 MB, 6.2 TB/s).  One launch whose
 // last slice of a row goes on to the gradient: 110 us, its workgroups' round trips follow one another.
+#include "dispatch.h"
 #include "dit.h"
 #include "train.h"
 
@@ -170,14 +171,12 @@ __global__ __launch_bounds__(OBJ_THREADS) void objective_grad_kernel(br_edge_set
   }
 }
 
-// Small sets in one launch of one workgroup, an edge, then a row, a wavefront at a time: the two launches above are 3 us each and 3 us of the host's.
-constexpr int OBJ_SMALL_EDGES = 512;
-constexpr long long OBJ_SMALL_VALUES = 1 << 15;
+// Small sets (rule::objective_one_launch) in one launch of one workgroup, an edge, then a row, a wavefront at a time.
 __global__ __launch_bounds__(1024) void objective_small_kernel(br_edge_set s, double inv_n, const float* __restrict__ z, const float* __restrict__ v,
                                                                const float* __restrict__ logp_old, const float* __restrict__ adv, float* __restrict__ J, float* __restrict__ logp_new,
                                                                float* __restrict__ grad, unsigned char* __restrict__ clipped) {
-  __shared__ double squares[OBJ_SMALL_EDGES], red[16];
-  __shared__ float weight[OBJ_SMALL_EDGES];
+  __shared__ double squares[rule::OBJECTIVE_SMALL_EDGES], red[16];
+  __shared__ float weight[rule::OBJECTIVE_SMALL_EDGES];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   for (int e = wave; e < s.n_edges; e += 16) {
     const ObjRow o = obj_row(s, z, v, obj_row_of(s, e));
@@ -230,7 +229,7 @@ br_status launch_objective_grad(const br_edge_set& e, const float* z, const floa
   BR_REQUIRE(n < 0x7FFFFFFFLL, BR_ESHAPE, "br_grpo_backward: too many rows for one launch");
   const double inv_n = 1.0 / (double)(e.n_total > 0 ? e.n_total : e.n_edges);
   double* part = reinterpret_cast<double*>(ws);
-  if (e.n_edges <= OBJ_SMALL_EDGES && (long long)e.n_edges * e.D <= OBJ_SMALL_VALUES) {
+  if (rule::objective_one_launch(e.n_edges, e.D)) {
     hipLaunchKernelGGL(objective_small_kernel, dim3(1), dim3(1024), 0, st, e, inv_n, z, v, logp_old, adv, J, logp_new, grad, clipped);
     BR_LAUNCH_CHECK();
     return BR_OK;

@@ -252,3 +252,14 @@ def test_offsets_of_thousands_of_documents_in_no_order_stay_inside():
     br.attention_forward(q, k, v, off, off, out, lse, ws)
     br.attention_backward(out, q, k, v, out, lse, off, off, dq, dk, dv, ws)
     assert np.all(host(big[:, :32]) == 7.0) and np.all(host(big[:, 32 + T:]) == 7.0) and np.all(host(big[:3]) == 7.0)
+
+
+# --------------------------------------------------------------------------------------- objective, one launch or two
+@pytest.mark.parametrize("T,splits,K,trees,D", [(8, (), 1, 2, 1536), (8, (), 1, 2, 1540), (16, (), 1, 2, 768), (16, (), 1, 2, 772), (11, (), 1, 3, 64), (2, (), 1, 3, 2560), (2, (), 1, 3, 2564), (1, (), 1, 1, 32768)])
+def test_objective_on_both_sides_of_its_one_launch(T, splits, K, trees, D):
+    """16 and 32 edges up to their line and past it, 33 edges, one edge of many values: log-densities, value and gradient against the oracle (bounds as in test_objective_and_its_gradient)."""
+    c = objective_case(T, splits, K, trees, D, 1.0, True, 1e-4, seed=D + T)
+    assert np.array_equal(c["clipped"], c["rclip"])
+    assert abs(c["J"] - c["rJ"]) <= 2.0 ** -20 * np.abs(c["adv"]).sum() / c["n"] * 8
+    w = np.array([np.abs(c["adv"][a:b]).sum() / c["n"] * 2 * h * abs(v) for a, b, (_, v, h, _) in zip(c["first"], c["first"][1:], c["coef"])])
+    assert np.all(np.abs(c["grad"] - c["rgrad"]) <= w[:, None] * 64 * 2.0 ** -22 + 1e-3 * 2.0 ** -10 * np.abs(c["rgrad"]))
