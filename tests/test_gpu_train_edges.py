@@ -10,7 +10,7 @@ from gpu_util import DEV, bytes_buffer, dev, host
 from oracle import objective, train
 from paper_2509_06040_amd import binding as br
 from paper_2509_06040_amd import synth
-from test_gpu_train_ops import Packed, norm_case, objective_case
+from test_gpu_train_ops import TYPES, Packed, norm_case, objective_case
 
 pytestmark = pytest.mark.gpu
 FORMS = [("bf16", 64), ("bf16", 128), ("f32", 16), ("f32", 64), ("f32", 128)]
@@ -277,3 +277,42 @@ def test_results_on_long_documents_by_their_norm(dtype, d, heads, kv_heads, lens
     refs, _ = train.attention_grad(do, q, k, v, p.q_off, p.k_off, p.scale)
     for name, t, ref in zip(("out", "dq", "dk", "dv"), (p.out, p.dq, p.dk, p.dv), (out, *refs)):
         assert off_by(host(t), ref) < (0.0027 if dtype == "bf16" else 1e-4), name
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 128), ("f32", 64)])
+def test_attention_at_the_length_of_a_video_sample(dtype, d):
+    """32 760 latent tokens and a prompt of 512, a short document in front and one behind; all log-sum-exps, and the output and gradients of 48 tokens, in 64 bits.  Norms bounded as above."""
+    lens, T = (77, 33272, 300), TYPES[dtype]
+    off = np.cumsum((0,) + lens)
+    q, k, v, do = (torch.randn(int(off[-1]), 1, d, device=DEV).to(T) for _ in range(4))
+    o, out, lse, grads = dev(off.astype(np.int32)), torch.empty_like(q), torch.empty(1, int(off[-1]), device=DEV), [torch.empty_like(q) for _ in range(3)]
+    ws = bytes_buffer(max(br.attention_workspace_bytes(q, k, v, o, o, b) for b in (False, True)))
+    br.attention_forward(q, k, v, o, o, out, lse, ws)
+    br.attention_backward(do, q, k, v, out, lse, o, o, *grads, ws)
+    a, b = int(off[1]), int(off[2])
+    scale = float(np.float32(1 / np.sqrt(d)))
+    Q, K, V, DO = (x[a:b, 0].double() for x in (q, k, v, do))
+    L, O = torch.empty(b - a, dtype=torch.float64, device=DEV), torch.empty(b - a, d, dtype=torch.float64, device=DEV)
+    for i in range(0, b - a, 4096):
+        s = Q[i:i + 4096] @ K.t().contiguous() * scale
+        L[i:i + 4096] = torch.logsumexp(s, 1)
+        O[i:i + 4096] = torch.exp(s - L[i:i + 4096, None]) @ V
+    assert float((lse[0, a:b].double() - L).abs().max()) < 1e-4
+    delta = (DO * O).sum(1)
+    at = torch.from_numpy(np.random.default_rng(d).choice(b - a, 48, replace=False)).to(DEV)
+    p = torch.exp(Q[at] @ K.t().contiguous() * scale - L[at, None])
+    dq = p * (DO[at] @ V.t().contiguous() - delta[at, None]) * scale @ K
+    p = torch.exp(Q @ K[at].t().contiguous() * scale - L[:, None])
+    ds = p * (DO @ V[at].t().contiguous() - delta[:, None]) * scale
+    refs = (O[at], dq, ds.t().contiguous() @ Q, p.t().contiguous() @ DO)
+    for name, got, ref in zip(("out", "dq", "dk", "dv"), (out, *grads), refs):
+        assert off_by(host(got)[a:b, 0][host(at)], host(ref)) < (0.0027 if dtype == "bf16" else 1e-4), name
+
+
+@pytest.mark.parametrize("D", [262144, 2096640])
+def test_objective_at_the_sizes_of_large_images_and_videos(D):
+    c = objective_case(4, (1, 2), 2, 1, D, 0.7, True, 1e-4, seed=1)
+    assert np.array_equal(c["clipped"], c["rclip"])
+    assert abs(c["J"] - c["rJ"]) <= 2.0 ** -20 * np.abs(c["adv"]).sum() / c["n"] * 8
+    w = np.array([np.abs(c["adv"][a:b]).sum() / c["n"] * 2 * h * abs(v) for a, b, (_, v, h, _) in zip(c["first"], c["first"][1:], c["coef"])])
+    assert np.all(np.abs(c["grad"] - c["rgrad"]) <= w[:, None] * 64 * 2.0 ** -22 + 1e-3 * 2.0 ** -10 * np.abs(c["rgrad"]))
