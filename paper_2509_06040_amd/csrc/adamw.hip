@@ -2,12 +2,12 @@
 // no table on the device.  A wavefront takes 256 consecutive elements of a tensor, four a lane: the block of one scale of
 // the states in 8 bits, whose largest value is then a maximum over the wavefront.
 //
-// 240 M parameters with bf16 gradients and copies: states in 32 bits 1150 us, 5.66 TB/s; in 8 bits 650 to 700 us, 5.4 to 5.8 TB/s, and the read-out of their values 407 us, 5.9.
+// 240 M parameters with bf16 gradients and copies: states in 32 bits 1150 us, 5.66 TB/s; in 8 bits 650 to 700 us (664 in a long run, 696 in the first passes of one), 5.4 to 5.8 TB/s, and the read-out of their values 411 us, 5.85.
 // A step in 8 bits has the chip's VALU nearly full (generator, root, quotient, codes): with scales by four quotients, maxima by way of LDS and codes taken apart with integer
 // arithmetic it took 747 to 812.
 //
-// Loads and stores of whole quads go past the caches, which nothing here is read from twice (states in 32 bits: plain 1223 us, stores past
-// them 1227, loads too 1151); the bf16 copies, which the network reads next, stay.
+// fp32 quads (parameters, gradients, states) are loaded and stored past the caches, and codes are stored so: nothing here is read twice (states in 32 bits: plain 1223 us, stores past
+// the caches 1227, loads too 1151).  bf16 gradients and codes are loaded plainly, bf16 copies, which the network reads next, stored so.
 //
 // Every product, sum, quotient and root is rounded by itself (no contraction): states in 8 bits are the same bits wherever they are computed.
 #include "dit.h"

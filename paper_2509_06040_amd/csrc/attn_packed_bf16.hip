@@ -10,9 +10,11 @@
 //
 // Bound by the matrix pipe, the exponentials issued beside it, and the clock that the chip's power leaves (2.0 to 2.3 GHz with random inputs; with inputs of zero
 // 20 to 30 % faster).  Measured: forward, 16 heads of 64, 16 documents of 1025 to 1101 tokens 96 us, 768 TFLOP/s (matrix pipe 32 % busy, VALU 54 %); backward of eight of them 155
-// us, 600 TFLOP/s by the formulas' five products, 840 by the seven; backward, 12 heads of 128, two documents of 4096 to 4608 728 us, 743 and 1041 (matrix pipe 51 % busy for
-// dq, 41 % for dk and dv, VALU 36 and 31 %); eight documents of 2001, 16 heads, forward 834 at heads of 64 and 1003 at 128, backward 1080 and
-// 1096 by the seven.  A library product of 8192^3 reaches 1202 on the same card.
+// us, 600 TFLOP/s by the formulas' five products, 840 by the seven; backward, 12 heads of 128, two documents of 4096 to 4608 716 to 737 us by machine, 735 to 755 and 1030 to 1060 (matrix pipe 52 % busy for
+// dq, 40 % for dk and dv, VALU 36 and 31 %); eight documents of 2001, 16 heads, forward 834 at heads of 64 and 1003 at 128, backward 1080 and
+// 1096 by the seven.  A library product of 8192^3 reaches 1570 on the same card, both operands along the contraction (1340 with the second as it lies, 1520 over large shapes).
+//
+// Rounded to bf16: P and dS, which the matrix instruction takes as bf16 operands, and the results; scores, sums, references and delta stay fp32.
 //
 // Tiles come straight from global memory into LDS, rows as they lie, 16-byte chunks permuted per row so that both the fragments of 16 rows
 // and the transposed reads (eight rows, two chunks) spread over the banks.
@@ -711,7 +713,8 @@ br_status launch_attn_grad_bf16(AttnArgs a, int parts_q, int parts_k, hipStream_
   return a.s.head_dim == 64 ? grad_launch<64>(a, parts_q, parts_k, st) : grad_launch<128>(a, parts_q, parts_k, st);
 }
 
-// Rows of a document are addressed with 32-bit byte offsets from its first one.
+// Rows of a document are addressed with 32-bit byte offsets from its first one; the host knows the matrices' size only.  Past it, eight documents of 1063 tokens, 16 heads of 64,
+// forward and backward: 94 and 249 us in the general form, 53 and 165 here.
 bool attn_packed_bf16_fits(const br_attn_shape& s) {
   auto fits = [](int64_t tokens, int64_t stride) { return tokens * stride * 2 < (1LL << 32); };
   return s.dtype == BR_BF16 && fits(s.q_tokens, s.q_stride) && fits(s.q_tokens, s.o_stride) && fits(s.k_tokens, s.k_stride) && fits(s.k_tokens, s.v_stride);
