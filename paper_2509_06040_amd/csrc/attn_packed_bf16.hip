@@ -579,26 +579,37 @@ static __device__ __forceinline__ void packed_grad_rows(const AttnArgs& a, const
       }
     };
     static_for<RA>([&](auto Nc) __attribute__((always_inline)) { fr[decltype(Nc)::value] = frag_of(Nc, 0, 0); });
-    u32x4 there;  // ones where the lane's rows of a head's last tile are below the end
+    u32x4 there;  // ones where the lane's queries of a head's last tile are below the end
+    if constexpr (KEYS) {
 #pragma unroll
-    for (int e = 0; e < 8; e += 2) {
-      const int row = (nt - 1) * PACK_TILE + (e >> 2) * 16 + 4 * g + (e & 3);
-      there[e >> 1] = (row < n_rows ? 0x0000FFFFu : 0u) | (row + 1 < n_rows ? 0xFFFF0000u : 0u);
+      for (int e = 0; e < 8; e += 2) {
+        const int row = (nt - 1) * PACK_TILE + (e >> 2) * 16 + 4 * g + (e & 3);
+        there[e >> 1] = (row < n_rows ? 0x0000FFFFu : 0u) | (row + 1 < n_rows ? 0xFFFF0000u : 0u);
+      }
     }
-    int j = 0, left = nt;
+    int j = 0, left = n_rows % PACK_TILE != 0 ? nt : -1;  // (tiles up to a head's last one, if that has rows past the end)
     bool more = true;
     while (more) {
       static_for<NB>([&](auto Bc) __attribute__((always_inline)) {
         if (!more) return;
         constexpr int B = decltype(Bc)::value, P = B & 1;
         step(std::integral_constant<int, P>{}, Bc);
-        if (--left == 0) {  // a head's last tile: rows past the end (zeros, which an infinite own row makes scores of that are not numbers) count as none
-          left = nt;
+        // rows past the end (zeros, which an infinite own row makes scores of that are not numbers) count as none
+        if constexpr (KEYS) {
+          if (--left == 0) {
+            left = nt;
 #pragma unroll
-          for (int qb = 0; qb < QB; ++qb) {
-            df[P][qb] &= there;
-            if constexpr (KEYS) pf[P][qb] &= there;
+            for (int qb = 0; qb < QB; ++qb) {
+              df[P][qb] &= there;
+              pf[P][qb] &= there;
+            }
           }
+        } else if (j == N - 1) {
+#pragma unroll
+          for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if (j * PACK_TILE + (e >> 2) * 16 + 4 * g + (e & 3) >= n_rows) df[P][qb][e >> 1] &= e & 1 ? 0x0000FFFFu : 0xFFFF0000u;
         }
         more = ++j < N;
         if (more) behind(Bc);
