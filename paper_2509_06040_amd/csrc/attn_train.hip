@@ -416,11 +416,16 @@ __global__ __launch_bounds__(256) void packed_attention_dkv_kernel(AttnArgs a) {
       const f32x4 ref = *reinterpret_cast<const f32x4*>(refs + (b0 + b) * 16 + 4 * g), delta = *reinterpret_cast<const f32x4*>(refs + TILE_ROWS + (b0 + b) * 16 + 4 * g);
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const float x = __builtin_amdgcn_exp2f(fmaf(p[b][r], unit, -ref[r]));
-        const bool in = (b0 + b) * 16 + 4 * g + r < there;
-        p[b][r] = in ? x : 0.f;
-        ds[b][r] = in ? x * (ds[b][r] + delta[r]) : 0.f;
+        p[b][r] = __builtin_amdgcn_exp2f(fmaf(p[b][r], unit, -ref[r]));
+        ds[b][r] = p[b][r] * (ds[b][r] + delta[r]);
       }
+    }
+    if (there < TILE_ROWS) {
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if ((b0 + b) * 16 + 4 * g + r >= there) p[b][r] = ds[b][r] = 0.f;
     }
 #pragma unroll
     for (int ks = 0; ks < PS; ++ks) {
